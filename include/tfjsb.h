@@ -80,6 +80,13 @@ typedef enum { TFJSB_ACT_NONE = 0, TFJSB_ACT_RELU = 1, TFJSB_ACT_RELU6 = 2 } tfj
  *         a multiple of 8), global avgPool, dense, softmax after dense.  The op entry points that
  *         take fp32 tensors run their FP32 path in this mode. */
 typedef enum { TFJSB_MATH_TF32 = 0, TFJSB_MATH_FP32 = 1, TFJSB_MATH_BF16 = 2 } tfjsb_math;
+/* Storage of the dense layers of transformer blocks below, which take plain pointers. */
+typedef enum { TFJSB_DTYPE_F32 = 0, TFJSB_DTYPE_BF16 = 1 } tfjsb_dtype;
+/* gate(g) of a gated feed-forward block: g s(g) with s(g) = 1 / (1 + exp(-g)); g F(g) with the normal distribution function
+ * F; g s(2 v) with v = sqrt(2 / pi) (g + 0.044715 g^3), which is g (1 + tanh v) / 2; s(g); max(g, 0), whose slope at 0 is 0. */
+typedef enum {
+    TFJSB_GATE_SILU = 0, TFJSB_GATE_GELU = 1, TFJSB_GATE_GELU_TANH = 2, TFJSB_GATE_SIGMOID = 3, TFJSB_GATE_RELU = 4
+} tfjsb_gate;
 typedef enum { TFJSB_BINARY_ADD = 0, TFJSB_BINARY_SUB = 1, TFJSB_BINARY_MUL = 2 } tfjsb_binary_op;
 
 /* ---- context ------------------------------------------------------------------------ */
@@ -260,6 +267,68 @@ tfjsb_status tfjsb_act_backprop(tfjsb_ctx* ctx, const tfjsb_tensor* y, const tfj
                                 tfjsb_tensor* dz, void* stream);
 /* dbias[c] = sum of dz[..., c] over every other dimension.  dz rank 1..4, dbias [last dim of dz]. */
 tfjsb_status tfjsb_bias_backprop(tfjsb_ctx* ctx, const tfjsb_tensor* dz, tfjsb_tensor* dbias, void* stream);
+
+/* ---- dense layers of transformer blocks --------------------------------------------------- */
+
+/* The paper's ops API serves whatever model is built from it (Sec. 3.3); it names matMul, not the layers below, whose formulas stand here.
+ * Tensors are DEVICE pointers to dense row-major values of the stated type, 16-byte aligned; outputs may alias neither inputs
+ * nor each other (dropout excepted).  Results do not depend on scheduling: the same call gives the same bits.  Workspaces are the
+ * caller's, 16-byte aligned, of at least the bytes that the *_sizes / *_workspace function gives; their contents mean nothing between calls.
+ * Calls whose workspaces and outputs are their own share nothing, so they can be captured into graphs of their own. */
+
+/* A gated feed-forward block: y = (gate(x w_gate) * (x w_up)) w_down, no biases.
+ *   x [tokens,width], w_gate and w_up [width,hidden], w_down [hidden,out_width], y [tokens,out_width], all of `dtype`.
+ * Any sizes from 1 to 2^30 (tokens may be 0); operands whose rows are no multiple of 16 bytes are copied into the workspace first.
+ * Products run on the tensor cores with fp32 sums: of bfloat16 values exactly, of fp32 values (as three bfloat16 parts) as exactly as
+ * fp32 multiply-adds; up to 8 tokens without a gradient on CUDA cores, which is where their weights can be read fastest.  In bfloat16,
+ * g = x w_gate and u = x w_up stay fp32, the product gate(g) u is rounded to bfloat16 once, and y once.  An infinity among fp32 operands
+ * may give NaN where the exact result is infinite. */
+typedef struct {
+    int64_t tokens, width, hidden, out_width;
+    int32_t dtype; /* tfjsb_dtype */
+    int32_t gate;  /* tfjsb_gate */
+} tfjsb_ffn;
+/* Bytes of what the forward pass keeps for the gradient (h, z) and of the workspaces of the two calls.  h holds gate(g) u, z holds g
+ * and u; their layouts are the library's own.  Any pointer may be NULL.  TFJSB_ERR_SHAPE / _INVALID_ARG for a shape that the calls refuse. */
+tfjsb_status tfjsb_gated_ffn_sizes(const tfjsb_ffn* ffn, int64_t* h_bytes, int64_t* z_bytes, int64_t* workspace_bytes,
+                                   int64_t* backprop_workspace_bytes);
+/* h and z: both (a gradient will be wanted) or neither (NULL). */
+tfjsb_status tfjsb_gated_ffn(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, const void* x, const void* w_gate, const void* w_up, const void* w_down, void* y,
+                             void* h, void* z, void* workspace, int64_t workspace_bytes, void* stream);
+/* The block's gradients, given that of y and what the forward pass kept: dx and those of the three weights, of `dtype`; those that are NULL are
+ * not computed.  The gradients of g and u are rounded to bfloat16 once where `dtype` is bfloat16.  With no tokens the weights' gradients are zero. */
+tfjsb_status tfjsb_gated_ffn_backprop(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, const void* x, const void* w_gate, const void* w_up, const void* w_down,
+                                      const void* h, const void* z, const void* dy, void* dx, void* dw_gate, void* dw_up, void* dw_down,
+                                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/* tf.dropout, from a counter-based generator: no mask is stored, the gradient makes it again.
+ *   out[i] = (keep[m(i)] ? x[i] / (1 - rate) : 0) + residual[i];  residual NULL: none.  A dropped value gives 0 whatever it was.
+ *   x, residual, out: rank 1..4, `dims`, of `dtype`; out may be x or residual.  noise_dims: NULL, or the mask's shape, of the same
+ *   rank, each dimension that of x or 1 (broadcast).  m(i) is the row-major index in the mask's shape.
+ *   keep[m] is word m % 4 of Philox-4x32-10 (Salmon et al. 2011) with key = seed and counter = (m / 4, offset), 64 bits each, low word
+ *   first: word >= ceil(rate 2^32).  0 <= rate < 1.
+ * The arithmetic is fp32, x * fp32(1 / (1 - rate)) + residual in one rounding, and one more into bfloat16.
+ * The gradient is the same call on dy without a residual (tfjsb_dropout_backprop). */
+tfjsb_status tfjsb_dropout(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, const void* residual, void* out, int32_t rank, const int64_t* dims,
+                           const int64_t* noise_dims, double rate, uint64_t seed, uint64_t offset, void* stream);
+tfjsb_status tfjsb_dropout_backprop(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* dy, void* dx, int32_t rank, const int64_t* dims,
+                                    const int64_t* noise_dims, double rate, uint64_t seed, uint64_t offset, void* stream);
+
+/* Rows of x [rows,columns] as 8-bit integers with a scale each: scale = max |x| / 127, q = 127 x / max |x| rounded to nearest,
+ * halves to even (decided exactly), so that q * scale is x to within half a step; a row of zeros has scale 0.  A row that holds an infinity or a NaN has that
+ * for a scale (NaN before infinity) and q = 0, so that products with it are NaN.  q: [rows, pitch] with pitch = columns rounded up to a
+ * multiple of 16, the values past the columns zero; scale: fp32 [rows].  columns <= 131072. */
+tfjsb_status tfjsb_quantize_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, void* stream);
+/* out[M,N] = act( (a[M,K] . bt[N,K]^T) * a_scale[M] * b_scale[N] + bias[N] ):  a and bt 8-bit integers with K contiguous (bt as matMul's right
+ * operand stored transposed), exact 32-bit sums, the rest in fp32, one more rounding where out is bfloat16.  a_scale, b_scale, bias fp32
+ * (bias may be NULL).  K a multiple of 16 (else TFJSB_ERR_UNSUPPORTED: fill rows up with zeros), at most 131072. */
+tfjsb_status tfjsb_matmul_int8(tfjsb_ctx* ctx, const int8_t* a, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias,
+                               tfjsb_act act, void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, void* stream);
+/* A dense layer on 8-bit weights: the two calls above on x [M,K] of `dtype`, with the same results.  bt is [N, K rounded up to a multiple of 16], the
+ * values past K zero (what is there is multiplied with zeros).  The workspace holds the rows' 8-bit values. */
+int64_t tfjsb_dense_int8_workspace(int64_t M, int64_t K);
+tfjsb_status tfjsb_dense_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, const int8_t* bt, const float* b_scale, const float* bias, tfjsb_act act,
+                              void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* ---- models ------------------------------------------------------------------------- */
 

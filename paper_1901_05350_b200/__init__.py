@@ -23,6 +23,7 @@ PAD = {"valid": 0, "same": 1}
 ACT = {"none": 0, "relu": 1, "relu6": 2}
 MATH = {"tf32": 0, "fp32": 1, "bf16": 2}
 BINARY_OP = {"add": 0, "sub": 1, "mul": 2}
+GATE = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "sigmoid": 3, "relu": 4}
 LAYER_KIND = {"conv2d": 0, "depthwise_conv2d": 1, "avg_pool": 2, "global_avg_pool": 2, "dense": 3, "softmax": 4}
 
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "SHAPE", 3: "UNSUPPORTED", 4: "CUDA", 5: "TIMEOUT", 6: "OOM"}
@@ -37,7 +38,8 @@ EXPORTS = [
     "tfjsb_matmul_bf16", "tfjsb_model_layer_output_f32", "tfjsb_model_layer_shape", "tfjsb_model_layer_kernel",
     "tfjsb_reserve_scratch", "tfjsb_conv2d_backprop_input", "tfjsb_conv2d_backprop_filter",
     "tfjsb_depthwise_conv2d_backprop_input", "tfjsb_depthwise_conv2d_backprop_filter", "tfjsb_act_backprop",
-    "tfjsb_bias_backprop",
+    "tfjsb_bias_backprop", "tfjsb_gated_ffn_sizes", "tfjsb_gated_ffn", "tfjsb_gated_ffn_backprop", "tfjsb_dropout",
+    "tfjsb_dropout_backprop", "tfjsb_quantize_int8", "tfjsb_matmul_int8", "tfjsb_dense_int8_workspace", "tfjsb_dense_int8",
 ]
 
 
@@ -50,6 +52,11 @@ class TfjsbError(RuntimeError):
 
 class Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("rank", ctypes.c_int32), ("dims", ctypes.c_int64 * 4)]
+
+
+class Ffn(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("width", ctypes.c_int64), ("hidden", ctypes.c_int64), ("out_width", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("gate", ctypes.c_int32)]
 
 
 class LayerDesc(ctypes.Structure):
@@ -117,6 +124,17 @@ def _load_library() -> ctypes.CDLL:
         getattr(lib, name).argtypes = [vp, tp, tp, ip, i32, ip, tp, vp]
     lib.tfjsb_act_backprop.argtypes = [vp, tp, tp, i32, tp, vp]
     lib.tfjsb_bias_backprop.argtypes = [vp, tp, tp, vp]
+    fp, ip64, u64, f64 = ctypes.POINTER(Ffn), ctypes.POINTER(i64), ctypes.c_uint64, ctypes.c_double
+    lib.tfjsb_gated_ffn_sizes.argtypes = [fp, ip64, ip64, ip64, ip64]
+    lib.tfjsb_gated_ffn.argtypes = [vp, fp] + [vp] * 8 + [i64, vp]
+    lib.tfjsb_gated_ffn_backprop.argtypes = [vp, fp] + [vp] * 12 + [i64, vp]
+    lib.tfjsb_dropout.argtypes = [vp, i32, vp, vp, vp, i32, ip64, ip64, f64, u64, u64, vp]
+    lib.tfjsb_dropout_backprop.argtypes = [vp, i32, vp, vp, i32, ip64, ip64, f64, u64, u64, vp]
+    lib.tfjsb_quantize_int8.argtypes = [vp, i32, vp, i64, i64, vp, vp, vp]
+    lib.tfjsb_matmul_int8.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, i32, i64, i64, i64, vp]
+    lib.tfjsb_dense_int8_workspace.argtypes = [i64, i64]
+    lib.tfjsb_dense_int8_workspace.restype = i64
+    lib.tfjsb_dense_int8.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, i32, i64, i64, i64, vp, i64, vp]
     return lib
 
 
@@ -180,6 +198,36 @@ def _stream() -> int:
     import torch
 
     return torch.cuda.current_stream().cuda_stream
+
+
+def _dtype(t) -> int:
+    """tfjsb_dtype of a tensor of the dense layers: fp32 or bfloat16."""
+    import torch
+
+    if t.dtype == torch.float32:
+        return 0
+    if t.dtype == torch.bfloat16:
+        return 1
+    raise TypeError("expected an fp32 or a bfloat16 tensor")
+
+
+def _plain(t, name: str, dtype, shape, device: int):
+    """Checks that `t` is a contiguous CUDA tensor on the context's device, of the dtype and the shape."""
+    import torch
+
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != device or t.dtype != dtype or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor on cuda:{device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, has {tuple(t.shape)}")
+    return t
+
+
+def _ptr(t):
+    return None if t is None or t.numel() == 0 else t.data_ptr()
+
+
+def _dims(shape) -> ctypes.Array:
+    return (ctypes.c_int64 * 4)(*[int(s) for s in shape])
 
 
 def _int2(v) -> ctypes.Array:
@@ -417,6 +465,186 @@ class Context:
             return done
         out = self._empty((dz.shape[-1],)) if out is None else out
         self._check(lib.tfjsb_bias_backprop(self._h, _desc(dz), _desc(out), _stream()))
+        return out
+
+    # -- dense layers of transformer blocks
+    def _stream_here(self) -> int:
+        import torch
+
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _new(self, shape, dtype):
+        import torch
+
+        return torch.empty(tuple(int(s) for s in shape), dtype=dtype, device=f"cuda:{self.device}")
+
+    def _bytes(self, count: int):
+        import torch
+
+        return self._new((max(int(count), 16),), torch.uint8)
+
+    def _ffn(self, x, w_gate, w_up, w_down, gate: str):
+        """The shape of a gated feed-forward call, with its tensors checked."""
+        import torch
+
+        if gate not in GATE:
+            raise ValueError(f"gate must be one of {', '.join(GATE)}")
+        for t, name in ((x, "x"), (w_gate, "w_gate"), (w_down, "w_down")):
+            if not isinstance(t, torch.Tensor) or t.dim() < (1 if name == "x" else 2):
+                raise TypeError(f"{name} must be a tensor of rank {'1 or more' if name == 'x' else 2}")
+        dtype = _dtype(x)
+        width, hidden, out_width = x.shape[-1], w_gate.shape[1], w_down.shape[1]
+        _plain(x, "x", x.dtype, x.shape, self.device)
+        _plain(w_gate, "w_gate", x.dtype, (width, hidden), self.device)
+        _plain(w_up, "w_up", x.dtype, (width, hidden), self.device)
+        _plain(w_down, "w_down", x.dtype, (hidden, out_width), self.device)
+        tokens = 1
+        for s in x.shape[:-1]:
+            tokens *= s
+        f = Ffn(tokens, width, hidden, out_width, dtype, GATE[gate])
+        sizes = (ctypes.c_int64 * 4)()
+        at = [ctypes.cast(ctypes.byref(sizes, 8 * i), ctypes.POINTER(ctypes.c_int64)) for i in range(4)]
+        rc = lib.tfjsb_gated_ffn_sizes(ctypes.byref(f), *at)
+        if rc:
+            raise TfjsbError(rc, f"no gated feed-forward block of {tokens} tokens, widths {width}, {hidden}, {out_width}")
+        return f, list(sizes)
+
+    def gated_ffn(self, x, w_gate, w_up, w_down, gate: str = "silu", save: bool = False, out=None):
+        """y = (gate(x w_gate) * (x w_up)) w_down: x [..., width], w_gate and w_up [width, hidden], w_down [hidden, out_width], all bfloat16
+        or all fp32; gate one of silu, gelu, gelu_tanh, sigmoid, relu.  With `save`, returns (y, h, z): what gated_ffn_backprop
+        needs besides its inputs (opaque)."""
+        if not save:
+            done = _fast.gated_ffn(self._fh, self.device, x, w_gate, w_up, w_down, GATE.get(gate, -1), out)
+            if done is not None:
+                return done
+        f, sizes = self._ffn(x, w_gate, w_up, w_down, gate)
+        shape = tuple(x.shape[:-1]) + (f.out_width,)
+        y = self._new(shape, x.dtype) if out is None else _plain(out, "out", x.dtype, shape, self.device)
+        h, z = (self._bytes(sizes[0]), self._bytes(sizes[1])) if save else (None, None)
+        # what the block itself takes for h where it is not saved is part of the workspace
+        work = self._bytes(sizes[2])
+        self._check(lib.tfjsb_gated_ffn(self._h, ctypes.byref(f), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(y), _ptr(h), _ptr(z),
+                                        work.data_ptr(), work.numel(), self._stream_here()))
+        return (y, h, z) if save else y
+
+    def gated_ffn_backprop(self, x, w_gate, w_up, w_down, h, z, dy, gate: str = "silu", want=(True, True, True, True)):
+        """(dx, dw_gate, dw_up, dw_down) of gated_ffn, given what it saved and the gradient of y; None for those not in `want`."""
+        import torch
+
+        f, sizes = self._ffn(x, w_gate, w_up, w_down, gate)
+        _plain(dy, "dy", x.dtype, tuple(x.shape[:-1]) + (f.out_width,), self.device)
+        for t, name, size in ((h, "h", sizes[0]), (z, "z", sizes[1])):
+            if not isinstance(t, torch.Tensor) or t.get_device() != self.device or t.dtype != torch.uint8 or t.numel() != max(size, 16):
+                raise ValueError(f"{name} is not what gated_ffn saved for these shapes")
+        if len(want) != 4:
+            raise ValueError("want has four entries")
+        grads = [self._new(t.shape, t.dtype) if w else None for t, w in zip((x, w_gate, w_up, w_down), want)]
+        work = self._bytes(sizes[3])
+        self._check(lib.tfjsb_gated_ffn_backprop(self._h, ctypes.byref(f), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(h), _ptr(z), _ptr(dy),
+                                                 *[_ptr(g) for g in grads], work.data_ptr(), work.numel(), self._stream_here()))
+        return tuple(grads)
+
+    def dropout(self, x, rate: float, seed: int, offset: int = 0, noise_shape=None, residual=None, out=None):
+        """tf.dropout: x / (1 - rate) where the mask keeps it, 0 elsewhere, plus `residual`.  The mask is a function of (seed, offset), whole
+        numbers of 64 bits, and of the place in it; `noise_shape` (x's shape, or 1 in some dimensions) broadcasts it.  `out` may be x or residual."""
+        done = _fast.dropout(self._fh, self.device, x, rate, seed, offset, noise_shape, residual, out)
+        if done is not None:
+            return done
+        return self._dropout(False, x, rate, seed, offset, noise_shape, residual, out)
+
+    def dropout_backprop(self, dy, rate: float, seed: int, offset: int = 0, noise_shape=None, out=None):
+        """The gradient of x, with the same mask made again: dropout of dy without a residual."""
+        done = _fast.dropout(self._fh, self.device, dy, rate, seed, offset, noise_shape, None, out)
+        if done is not None:
+            return done
+        return self._dropout(True, dy, rate, seed, offset, noise_shape, None, out)
+
+    def _dropout(self, backprop, x, rate, seed, offset, noise_shape, residual, out):
+        import torch
+
+        if not isinstance(x, torch.Tensor):
+            raise TypeError("expected a tensor")
+        dtype = _dtype(x)
+        _plain(x, "dy" if backprop else "x", x.dtype, x.shape, self.device)
+        if residual is not None:
+            _plain(residual, "residual", x.dtype, x.shape, self.device)
+        if noise_shape is not None and len(noise_shape) != x.dim():
+            raise ValueError("noise_shape must have x's rank")
+        for v, name in ((seed, "seed"), (offset, "offset")):
+            if int(v) != v or not 0 <= v < 2 ** 64:
+                raise ValueError(f"{name} must be a whole number from 0 to 2^64 - 1")
+        if not 1 <= x.dim() <= 4:
+            raise ValueError("expected a tensor of rank 1..4")
+        out = self._new(x.shape, x.dtype) if out is None else _plain(out, "out", x.dtype, x.shape, self.device)
+        noise = None if noise_shape is None else _dims(noise_shape)
+        if backprop:
+            self._check(lib.tfjsb_dropout_backprop(self._h, dtype, _ptr(x), _ptr(out), x.dim(), _dims(x.shape), noise, rate, seed, offset, self._stream_here()))
+        else:
+            self._check(lib.tfjsb_dropout(self._h, dtype, _ptr(x), _ptr(residual), _ptr(out), x.dim(), _dims(x.shape), noise, rate, seed, offset,
+                                          self._stream_here()))
+        return out
+
+    def quantize_int8(self, x):
+        """(q, scale) of the rows of x [rows, columns], bfloat16 or fp32: q int8 [rows, columns rounded up to a multiple of 16] (zeros past
+        the columns), scale fp32 [rows], q * scale = x to half a step.  A dense layer's weights [outputs, inner] are laid out with it too."""
+        import torch
+
+        if not isinstance(x, torch.Tensor) or x.dim() != 2:
+            raise TypeError("x must be a tensor of rank 2")
+        dtype = _dtype(x)
+        _plain(x, "x", x.dtype, x.shape, self.device)
+        rows, columns = x.shape
+        q = self._new((rows, -(-columns // 16) * 16), torch.int8)
+        scale = self._new((rows,), torch.float32)
+        self._check(lib.tfjsb_quantize_int8(self._h, dtype, _ptr(x), rows, columns, _ptr(q), _ptr(scale), self._stream_here()))
+        return q, scale
+
+    def _int8_rest(self, M, N, bt_scale, bias, out_dtype, out):
+        """Checks what both 8-bit products take; (out, its tfjsb_dtype)."""
+        import torch
+
+        _plain(bt_scale, "bt_scale", torch.float32, (N,), self.device)
+        if bias is not None:
+            _plain(bias, "bias", torch.float32, (N,), self.device)
+        out = self._new((M, N), out_dtype) if out is None else _plain(out, "out", out.dtype, (M, N), self.device)
+        return out, _dtype(out)
+
+    def matmul_int8(self, a, a_scale, bt, bt_scale, bias=None, act="none", out_dtype=None, out=None):
+        """act((a . bt^T) * a_scale[:, None] * bt_scale + bias): a [M,K] and bt [N,K] int8 with K a multiple of 16 (quantize_int8 fills
+        rows up), scales and bias fp32; exact 32-bit sums; the result bfloat16 (default) or fp32."""
+        import torch
+
+        for t, name in ((a, "a"), (bt, "bt")):
+            if not isinstance(t, torch.Tensor) or t.dim() != 2:
+                raise TypeError(f"{name} must be a tensor of rank 2")
+        M, K, N = a.shape[0], a.shape[1], bt.shape[0]
+        _plain(a, "a", torch.int8, (M, K), self.device)
+        _plain(bt, "bt", torch.int8, (N, K), self.device)
+        _plain(a_scale, "a_scale", torch.float32, (M,), self.device)
+        out, dtype = self._int8_rest(M, N, bt_scale, bias, out_dtype or torch.bfloat16, out)
+        self._check(lib.tfjsb_matmul_int8(self._h, _ptr(a), _ptr(a_scale), _ptr(bt), _ptr(bt_scale), _ptr(bias), ACT[act], _ptr(out), dtype, M, N, K,
+                                          self._stream_here()))
+        return out
+
+    def dense_int8(self, x, bt, bt_scale, bias=None, act="none", out_dtype=None, out=None):
+        """A dense layer on 8-bit weights, act(q(x) . w + bias): x [M,K] bfloat16 or fp32, its rows quantised as quantize_int8 does; bt
+        [N, K rounded up to a multiple of 16] and bt_scale [N] as quantize_int8 lays them out; bias fp32 [N] or None; the result in
+        x's dtype unless told otherwise."""
+        done = _fast.dense_int8(self._fh, self.device, x, bt, bt_scale, bias, ACT[act], out_dtype, out)
+        if done is not None:
+            return done
+        import torch
+
+        if not isinstance(x, torch.Tensor) or x.dim() != 2 or not isinstance(bt, torch.Tensor) or bt.dim() != 2:
+            raise TypeError("x and bt must be tensors of rank 2")
+        dtype = _dtype(x)
+        M, K, N = x.shape[0], x.shape[1], bt.shape[0]
+        _plain(x, "x", x.dtype, (M, K), self.device)
+        _plain(bt, "bt", torch.int8, (N, -(-K // 16) * 16), self.device)
+        out, to = self._int8_rest(M, N, bt_scale, bias, out_dtype or x.dtype, out)
+        work = self._bytes(lib.tfjsb_dense_int8_workspace(M, K))
+        self._check(lib.tfjsb_dense_int8(self._h, dtype, _ptr(x), _ptr(bt), _ptr(bt_scale), _ptr(bias), ACT[act], _ptr(out), to, M, N, K,
+                                         work.data_ptr(), work.numel(), self._stream_here()))
         return out
 
     def model(self, layers: Sequence, input_shape) -> "Model":

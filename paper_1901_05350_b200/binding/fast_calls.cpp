@@ -25,7 +25,7 @@ namespace {
     X(tfjsb_binary) X(tfjsb_softmax) X(tfjsb_bias_act) X(tfjsb_conv2d_backprop_input) X(tfjsb_conv2d_backprop_filter)         \
     X(tfjsb_depthwise_conv2d_backprop_input) X(tfjsb_depthwise_conv2d_backprop_filter) X(tfjsb_act_backprop)                  \
     X(tfjsb_bias_backprop) X(tfjsb_run_model) X(tfjsb_model_layer_output_f32) X(tfjsb_model_layer_shape) X(tfjsb_window_out_shape)       \
-    X(tfjsb_last_error)
+    X(tfjsb_last_error) X(tfjsb_gated_ffn_sizes) X(tfjsb_gated_ffn) X(tfjsb_dropout) X(tfjsb_dense_int8_workspace) X(tfjsb_dense_int8)
 #define DECLARE(name) decltype(&::name) p_##name = nullptr;
 FAST_CALLS(DECLARE)
 #undef DECLARE
@@ -385,6 +385,149 @@ PyObject* layer_output_f32(Args& a) {
     return out.done(h.ctx, unlocked([&] { return p_tfjsb_model_layer_output_f32(m, layer, static_cast<float*>(out.desc.data), s); }));
 }
 
+// ---- dense layers of transformer blocks: contiguous tensors of fp32 or bfloat16 on the context's device ----
+
+// A tensor of such a call; `dtype` receives its tfjsb_dtype, or has to agree with it when it is not negative.
+const at::Tensor* dense_tensor(Args& a, int device, int* dtype) {
+    PyObject* o = a.next();
+    if (!o || !THPVariable_Check(o)) { a.ok = false; return nullptr; }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    const int is = t.scalar_type() == at::kFloat ? TFJSB_DTYPE_F32 : t.scalar_type() == at::kBFloat16 ? TFJSB_DTYPE_BF16 : -1;
+    if (is < 0 || (*dtype >= 0 && *dtype != is) || !t.is_cuda() || t.get_device() != device || !t.is_contiguous()) { a.ok = false; return nullptr; }
+    *dtype = is;
+    return &t;
+}
+bool has_shape(const at::Tensor& t, int64_t rows, int64_t columns) { return t.dim() == 2 && t.size(0) == rows && t.size(1) == columns; }
+at::TensorBase new_tensor(at::IntArrayRef shape, at::ScalarType type, int device) {
+    return at::detail::empty_cuda(shape, type, at::Device(at::kCUDA, (at::DeviceIndex)device), std::nullopt);
+}
+at::ScalarType scalar_of(int dtype) { return dtype == TFJSB_DTYPE_F32 ? at::kFloat : at::kBFloat16; }
+
+// The output of such a call: the tensor that the caller passed, which has to have the shape, or a new one.
+struct DenseOut {
+    PyObject* given = nullptr;
+    at::TensorBase made;
+    void* data = nullptr;
+    void take(Args& a, int device, at::IntArrayRef shape, int* dtype) {
+        if (!a.ok) return;
+        if (*a.at == Py_None) {
+            ++a.at;
+            made = new_tensor(shape, scalar_of(*dtype), device);
+            data = const_cast<void*>(made.const_data_ptr());
+            return;
+        }
+        given = *a.at;
+        const at::Tensor* t = dense_tensor(a, device, dtype);
+        if (!t || t->sizes() != shape) { a.ok = false; return; }
+        data = const_cast<void*>(t->const_data_ptr());
+    }
+    PyObject* done(tfjsb_ctx* ctx, tfjsb_status st) {
+        Out o;
+        o.given = given;
+        o.made = std::move(made);
+        return o.done(ctx, st);
+    }
+};
+
+// gated_ffn(ctx, device, x, w_gate, w_up, w_down, gate, out)
+PyObject* gated_ffn(Args& a) {
+    const Head h(a);
+    int dtype = -1;
+    const at::Tensor* t[4];
+    for (auto& p : t) {
+        p = dense_tensor(a, h.device, &dtype);
+        if (!p) Py_RETURN_NONE;
+    }
+    const int gate = (int)a.integer();
+    const at::Tensor& x = *t[0];
+    if (!a.ok || x.dim() < 1 || x.dim() > 8 || t[1]->dim() != 2 || t[3]->dim() != 2) Py_RETURN_NONE;
+    const int64_t width = x.size(-1), hidden = t[1]->size(1), out_width = t[3]->size(1);
+    if (width < 1 || !has_shape(*t[1], width, hidden) || !has_shape(*t[2], width, hidden) || !has_shape(*t[3], hidden, out_width)) Py_RETURN_NONE;
+    const tfjsb_ffn f = {x.numel() / width, width, hidden, out_width, dtype, gate};
+    int64_t bytes = 0;
+    if (f.tokens < 1 || p_tfjsb_gated_ffn_sizes(&f, nullptr, nullptr, &bytes, nullptr) != TFJSB_OK) Py_RETURN_NONE;
+    int64_t shape[8];
+    for (int64_t i = 0; i < x.dim(); ++i) shape[i] = x.size(i);
+    shape[x.dim() - 1] = out_width;
+    DenseOut out;
+    out.take(a, h.device, at::IntArrayRef(shape, x.dim()), &dtype);
+    if (!a.ok) Py_RETURN_NONE;
+    const at::TensorBase work = new_tensor({bytes}, at::kByte, h.device);
+    void* s = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)h.device).stream();
+    return out.done(h.ctx, unlocked([&] {
+        return p_tfjsb_gated_ffn(h.ctx, &f, x.const_data_ptr(), t[1]->const_data_ptr(), t[2]->const_data_ptr(), t[3]->const_data_ptr(), out.data, nullptr,
+                                 nullptr, const_cast<void*>(work.const_data_ptr()), bytes, s);
+    }));
+}
+
+// dropout(ctx, device, x, rate, seed, offset, noise shape or None, residual or None, out)
+PyObject* dropout(Args& a) {
+    const Head h(a);
+    int dtype = -1;
+    const at::Tensor* x = dense_tensor(a, h.device, &dtype);
+    PyObject* rate = a.next();
+    if (!x || !rate || !PyFloat_CheckExact(rate) || x->dim() < 1 || x->dim() > 4 || x->numel() == 0) Py_RETURN_NONE;
+    uint64_t word[2];
+    for (auto& w : word) {
+        PyObject* o = a.next();
+        if (!o || !PyLong_CheckExact(o)) Py_RETURN_NONE;
+        w = PyLong_AsUnsignedLongLong(o);
+        if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+    }
+    int64_t noise[4];
+    const bool shared = a.ok && *a.at != Py_None;
+    if (!shared) ++a.at;
+    else if (a.integers(noise, (int)x->dim()) != x->dim()) Py_RETURN_NONE;
+    if (!a.ok) Py_RETURN_NONE;
+    const at::Tensor* residual = nullptr;
+    if (*a.at == Py_None) ++a.at;
+    else if (!(residual = dense_tensor(a, h.device, &dtype)) || residual->sizes() != x->sizes()) Py_RETURN_NONE;
+    DenseOut out;
+    out.take(a, h.device, x->sizes(), &dtype);
+    if (!a.ok) Py_RETURN_NONE;
+    void* s = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)h.device).stream();
+    const double r = PyFloat_AS_DOUBLE(rate);
+    return out.done(h.ctx, unlocked([&] {
+        return p_tfjsb_dropout(h.ctx, (tfjsb_dtype)dtype, x->const_data_ptr(), residual ? residual->const_data_ptr() : nullptr, out.data, (int32_t)x->dim(),
+                               x->sizes().data(), shared ? noise : nullptr, r, word[0], word[1], s);
+    }));
+}
+
+// dense_int8(ctx, device, x, bt, bt_scale, bias or None, act, out dtype (None: x's), out)
+PyObject* dense_int8(Args& a) {
+    const Head h(a);
+    int dtype = -1, f32 = TFJSB_DTYPE_F32;
+    const at::Tensor* x = dense_tensor(a, h.device, &dtype);
+    PyObject* o = a.next();
+    if (!x || x->dim() != 2 || !o || !THPVariable_Check(o)) Py_RETURN_NONE;
+    const at::Tensor& bt = THPVariable_Unpack(o);
+    const int64_t M = x->size(0), K = x->size(1);
+    if (M < 1 || K < 1 || bt.scalar_type() != at::kChar || !bt.is_cuda() || bt.get_device() != h.device || !bt.is_contiguous() || bt.dim() != 2 ||
+        bt.size(1) != (K + 15) / 16 * 16)
+        Py_RETURN_NONE;
+    const int64_t N = bt.size(0);
+    const at::Tensor* scale = dense_tensor(a, h.device, &f32);
+    if (!scale || scale->dim() != 1 || scale->size(0) != N || N < 1) Py_RETURN_NONE;
+    const at::Tensor* bias = nullptr;
+    if (*a.at == Py_None) ++a.at;
+    else if (!(bias = dense_tensor(a, h.device, &f32)) || bias->dim() != 1 || bias->size(0) != N) Py_RETURN_NONE;
+    const int act = (int)a.integer();
+    if (!a.ok || a.next() != Py_None) Py_RETURN_NONE;
+    int to = dtype;
+    DenseOut out;
+    if (*a.at != Py_None) to = -1;  // the dtype of the tensor that is given
+    out.take(a, h.device, {M, N}, &to);
+    const int64_t bytes = p_tfjsb_dense_int8_workspace(M, K);
+    if (!a.ok || bytes < 1) Py_RETURN_NONE;
+    const at::TensorBase work = new_tensor({bytes}, at::kByte, h.device);
+    void* s = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)h.device).stream();
+    return out.done(h.ctx, unlocked([&] {
+        return p_tfjsb_dense_int8(h.ctx, (tfjsb_dtype)dtype, x->const_data_ptr(), static_cast<const int8_t*>(bt.const_data_ptr()),
+                                  static_cast<const float*>(scale->const_data_ptr()), bias ? static_cast<const float*>(bias->const_data_ptr()) : nullptr,
+                                  (tfjsb_act)act, out.data, (tfjsb_dtype)to, M, N, K, const_cast<void*>(work.const_data_ptr()), bytes, s);
+    }));
+}
+
 #define METHOD(name, op, n) {name, (PyCFunction)(void (*)(void))(&entry<op, n>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, nullptr},
@@ -402,6 +545,9 @@ PyMethodDef methods[] = {
     METHOD("bias_backprop", bias_backprop, 4),
     METHOD("run_model", run_model, 6),
     METHOD("layer_output_f32", layer_output_f32, 4),
+    METHOD("gated_ffn", gated_ffn, 8),
+    METHOD("dropout", dropout, 9),
+    METHOD("dense_int8", dense_int8, 9),
     {nullptr, nullptr, 0, nullptr},
 };
 #undef METHOD

@@ -40,6 +40,10 @@ SOURCES = [
     "conv_patch_tcgen05.cu",
     "gemm_strided_tcgen05.cu",
     "chain_cluster.cu",
+    "dense_tcgen05.cu",
+    "gated_ffn.cu",
+    "dropout.cu",
+    "int8_dense.cu",
 ]
 
 NVCC_FLAGS = [

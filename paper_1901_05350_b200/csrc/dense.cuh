@@ -1,0 +1,72 @@
+// Shared by the dense layers of transformer blocks: the tensor-core product with their epilogues (dense_tcgen05.cu), the gated
+// feed-forward block (gated_ffn.cu) and the 8-bit dense layer (int8_dense.cu).
+#pragma once
+
+#include "common.cuh"
+
+namespace tfjsb {
+namespace dense {
+
+// What an operand's planes are: one plane of bfloat16 or 8-bit values, or an fp32 matrix as three bfloat16 planes whose sum
+// it is (8 + 8 + 8 significant bits, so the sum is exact).
+enum Kind { KIND_BF16 = 0, KIND_INT8 = 1 };
+// What becomes of the sums of a tile.
+enum Epilogue {
+    EPI_STORE,  // written as they are: bfloat16 (one plane) or fp32 (three)
+    EPI_GATED,  // columns come in pairs (g, u) from two weights: h = gate(g) u, and (g, u) themselves where `z` is given
+    EPI_GRAD,   // sums are dh: with g and u read from `z`, dg = dh u gate'(g) and du = dh gate(g)
+    EPI_SCALE,  // 32-bit integers: act(sum a_scale[row] b_scale[column] + bias[column]) in bfloat16 or fp32
+};
+
+// A stored operand.  K-contiguous: [outer rows][K]; otherwise `mn`: [K][rows].  `pitch` in elements, a multiple of 16 bytes.
+struct Operand {
+    const void* base = nullptr;
+    int64_t pitch = 0;   // between rows of memory
+    int64_t plane = 0;   // between planes, in elements (any when there is one)
+    int planes = 1;
+    bool mn = false;
+};
+
+struct Args {
+    int M = 0, N = 0, K = 0;      // of one pass; N: columns of one output (of h for EPI_GATED)
+    int block_n = 0, stages = 0, acc_stages = 0;
+    int n_tiles = 0, m_tiles = 0, outputs = 1, num_tiles = 0, band = 8;
+    int passes = 1, num_kb = 0, kb_per_split = 0, seg_kb = 0;
+    int splits = 1;
+    int a_mn = 0, b_mn = 0, a_rows = 0;
+    void* out[2] = {nullptr, nullptr};
+    int64_t out_pitch = 0, out_plane = 0;  // elements
+    float* z = nullptr;                    // [2][M][z_pitch]
+    int64_t z_pitch = 0;
+    int gate = 0;
+    int out_bf16 = 1, act = 0;             // EPI_SCALE
+    const float *a_scale = nullptr, *b_scale = nullptr, *bias = nullptr;
+    unsigned int* dev_status = nullptr;
+};
+
+// C = A B summed over `passes` pairs (plane group p of A with b[p]), or with `outputs` = 2 the products of A with the two
+// plane groups of b[0]; EPI_GATED: A with b[0] and b[1].  Fill in args.{M, N, K, passes, outputs, out*, z*, gate, ...}.
+struct Product {
+    Kind kind = KIND_BF16;
+    int planes = 1;
+    Epilogue epilogue = EPI_STORE;
+    Operand a, b[2];
+    Args args;
+};
+tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s);
+
+// The context's device is the current one while this lives: tensors say where they are, the caller's device may be another.
+struct OnDevice {
+    int before = -1;
+    explicit OnDevice(const tfjsb_ctx* ctx) {
+        int now = -1;
+        if (cudaGetDevice(&now) == cudaSuccess && now != ctx->device && cudaSetDevice(ctx->device) == cudaSuccess) before = now;
+    }
+    ~OnDevice() {
+        if (before >= 0) cudaSetDevice(before);
+    }
+    OnDevice(const OnDevice&) = delete;
+};
+
+}  // namespace dense
+}  // namespace tfjsb

@@ -1,0 +1,674 @@
+// Tensor-core products of the dense layers of transformer blocks: bfloat16 operands (tcgen05 kind::f16), fp32 operands as three
+// bfloat16 planes each, or 8-bit integers (kind::i8), with the layers' own epilogues.
+//
+//     sum[M,N] = sum over passes p and k of  A_p[M,K] B_p[K,N]
+//
+// Operands are read as they are stored: with K contiguous (128-byte-swizzled rows of 128 bytes) or with rows or columns
+// contiguous (boxes of 64 k x 64 columns in the same swizzle).  A k-block is 128 bytes of K: 64 bfloat16 or 128 8-bit values,
+// four MMAs.  The gated block's two projections are ONE product: half of a tile's columns come from Wg and half from Wu, so that g and u of
+// an element are in the same tensor-memory lane and h = gate(g) u needs no exchange; in a CTA pair each CTA fetches the
+// columns of one of them.  The gradient of x is one product too, over dg Wg^T and then du Wu^T in the same accumulator, and the
+// gradients of Wg and Wu are one launch over the tiles of both.
+//
+// Structure (CTA pairs, CG = 2, as in gemm_pair.cu; single CTAs, CG = 1, without the cluster): warp 0 copies (TMA), warp 1 issues the
+// MMAs, warps 2-9 are the epilogue, which works on one accumulator stage while the next tile is summed in the other.  The epilogue writes
+// global memory directly: a thread has a row, 32 bytes of it at a time, so that every sector is written once and whole.
+// Persistent over tiles in bands of `band` tile rows, so that the tiles in flight share operand rows and columns in L2.
+//
+// Few tiles: K is cut among the CTAs of a cluster (CG = 1, one tile each).  Each writes its partial tile to its own shared
+// memory, and after a cluster barrier every CTA adds the parts of its share of the tile in the order of the slices, from
+// distributed shared memory, and runs the epilogue on them.  No atomics: results do not depend on scheduling.
+//
+// fp32: v = p0 + p1 + p2 (bfloat16, rounded to nearest each, exact), a b = p0 q0 + (p0 q1 + p1 q0 + p1 q1 + p0 q2 + p2 q0), what is left out is
+// below 2^-26 of it.  The tensor core cuts every sum towards zero, so the error of an accumulator grows with the number of
+// additions: the large products go to an accumulator of their own for `seg_kb` k-blocks only (8 additions), the small ones
+// to another, and the epilogue adds both to fp32 sums in registers, rounded to nearest.
+#include <cstdlib>
+
+#include <cuda_bf16.h>
+
+#include "dense.cuh"
+#include "dense_math.cuh"
+#include "ptx_sm100.cuh"
+#include "umma_tile.cuh"
+
+namespace tfjsb {
+namespace dense {
+
+using namespace ptx;
+using tile::give_up;
+using tile::drain;
+
+namespace {
+
+constexpr int THREADS = 320;  // producer warp, MMA warp, 8 epilogue warps
+constexpr int MAX_STAGES = 8;
+constexpr int ROWS = 128;     // of a CTA's tile
+constexpr int A_BYTES = ROWS * 128;
+constexpr int GROUP_BYTES = 64 * 128;  // a box of 64 k x 64 columns
+
+// Operand tile whose memory runs along M or N: descriptor of boxes of 64 columns x 64 k in the 128-byte swizzle.  Eight k are
+// 1024 bytes (stride byte offset), groups of 64 columns 8192 bytes apart (leading byte offset); an MMA's 16 k are 2048 bytes.
+__device__ __forceinline__ uint64_t mn_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(GROUP_BYTES >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) |
+           (2ull << 61);
+}
+
+template <int CG, int KIND>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    if (KIND == KIND_BF16) {
+        if (CG == 2)
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+                         "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        else
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+                         "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    } else {
+        if (CG == 2)
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+                         "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        else
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+                         "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void commit(uint32_t bar) {  // to this CTA, or to the same barrier of both
+    if (CG == 2) tc_commit_pair(bar, (uint16_t)3);
+    else tc_commit(bar);
+}
+// Copy whose bytes are counted on `bar`: of this CTA, or (CG = 2) a shared::cluster address of the even one.
+template <int CG>
+__device__ __forceinline__ void load3(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+    if (CG == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+            "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+    else tma_load_3d(dst, map, bar, c0, c1, c2);
+}
+
+__device__ __forceinline__ uint4 lds4_cluster(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+// Tile number -> (tile row, tile column), in bands of `band` tile rows, down a band's columns one after the other.
+__device__ __forceinline__ void tile_at(const Args& a, int tile, int* m, int* n) {
+    const int columns = a.n_tiles * a.outputs;
+    const int per_band = a.band * columns;
+    const int b = tile / per_band, in = tile - b * per_band;
+    const int rows = min(a.band, a.m_tiles - b * a.band);
+    *n = in / rows;
+    *m = b * a.band + in - *n * rows;
+}
+
+// ---- what becomes of W sums of a row -------------------------------------------------------------------
+// `first` and, for EPI_GATED, `second` are the sums (g and u) of columns col .. col + W - 1 of row `row`; W is 8 or 32.
+template <int P, int EPI, int W>
+__device__ __forceinline__ void finish(const Args& a, int which, int64_t row, int col, const uint32_t (&first)[W], const uint32_t (&second)[W]) {
+    const int left = a.N - col;  // columns that exist
+    if (row >= a.M || left <= 0) return;
+    float v[W];
+    if constexpr (EPI == EPI_STORE) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = __uint_as_float(first[i]);
+        if constexpr (P == 1) store_bf16(static_cast<__nv_bfloat16*>(a.out[which]) + row * a.out_pitch + col, v, left);
+        else store_f32(static_cast<float*>(a.out[which]) + row * a.out_pitch + col, v, left);
+    } else if constexpr (EPI == EPI_SCALE) {
+        const float s = load_global(a.a_scale + row);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if (i < left) {
+                float r = (float)(int)first[i] * s * load_global(a.b_scale + col + i);
+                if (a.bias) r += load_global(a.bias + col + i);
+                v[i] = apply_act(r, a.act);
+            } else {
+                v[i] = 0.f;
+            }
+        }
+        if (a.out_bf16) store_bf16(static_cast<__nv_bfloat16*>(a.out[0]) + row * a.out_pitch + col, v, left);
+        else store_f32(static_cast<float*>(a.out[0]) + row * a.out_pitch + col, v, left);
+    } else if constexpr (EPI == EPI_GATED) {
+        float g[W], u[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) { g[i] = __uint_as_float(first[i]); u[i] = __uint_as_float(second[i]); }
+        if (a.z) {
+            float* z = a.z + row * a.z_pitch + col;
+            store_f32(z, g, left);
+            store_f32(z + (int64_t)a.M * a.z_pitch, u, left);
+        }
+        gated<P == 3>(a.gate, g, u, v);
+        store_planes<P>(static_cast<__nv_bfloat16*>(a.out[0]) + row * a.out_pitch + col, a.out_plane, v, left);
+    } else {
+        float g[W], u[W], du[W];
+        const float* z = a.z + row * a.z_pitch + col;
+        load_f32(z, g, left);
+        load_f32(z + (int64_t)a.M * a.z_pitch, u, left);
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = __uint_as_float(first[i]);
+        gated_gradient<P == 3>(a.gate, g, u, v, du);  // v: dh -> dg
+        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out[0]) + row * a.out_pitch + col;
+        store_planes<P>(dst, a.out_plane, v, left);
+        store_planes<P>(dst + P * a.out_plane, a.out_plane, du, left);
+    }
+}
+
+template <int CG, int P, int KIND, int EPI>
+__global__ void __launch_bounds__(THREADS, 1)
+dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1,
+             const __grid_constant__ Args args) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bar_full[MAX_STAGES];  // CG = 2: used in the even CTA only
+    __shared__ __align__(8) uint64_t bar_empty[MAX_STAGES];
+    __shared__ __align__(8) uint64_t bar_acc_full[2];
+    __shared__ __align__(8) uint64_t bar_acc_empty[2];      // CG = 2: used in the even CTA only
+    __shared__ __align__(8) uint64_t bar_drain;
+    __shared__ uint32_t tmem_base_slot;
+    __shared__ int abort_flag_s;
+
+    volatile int* abort_flag = &abort_flag_s;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_ctarank() : 0u;
+    const uint32_t slice = CG == 1 && args.splits > 1 ? cluster_ctarank() : 0u;
+    const bool leader = rank == 0;
+    const int block_n = args.block_n, stages = args.stages;
+    const int own_n = block_n / CG;  // columns of B that this CTA fetches
+    const uint32_t a_plane = A_BYTES, b_plane = (uint32_t)own_n * 128u;
+    const uint32_t stage_bytes = P * (a_plane + b_plane);
+    const uint32_t tx_bytes = CG * P * ((uint32_t)args.a_rows * 128u + b_plane);
+    const int first_tile = args.splits > 1 ? (int)blockIdx.x / args.splits : (int)blockIdx.x / CG;
+    const int tile_step = args.splits > 1 ? args.num_tiles : (int)gridDim.x / CG;  // a slice has one tile
+    const int kb_total = args.passes * args.num_kb;
+    const int kb_begin = (int)slice * args.kb_per_split;
+    const int kb_end = args.splits > 1 ? min(kb_total, kb_begin + args.kb_per_split) : kb_total;
+    constexpr int BK = KIND == KIND_BF16 ? 64 : 128;
+    const uint32_t acc_cols = (uint32_t)block_n * (P == 3 ? 2u : 1u);  // of an accumulator stage: large | small
+    const uint32_t stage_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < stages; ++s) {
+            mbar_init(smem_u32(&bar_full[s]), 1);
+            mbar_init(smem_u32(&bar_empty[s]), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(smem_u32(&bar_acc_full[s]), 1);
+            mbar_init(smem_u32(&bar_acc_empty[s]), 8 * CG);  // the epilogue warps
+        }
+        mbar_init(smem_u32(&bar_drain), 1);
+        abort_flag_s = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b0) : "memory");
+    }
+    constexpr uint32_t TMEM_COLS = 512;
+    if (warp == 1) {
+        if (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) {  // the partner's barriers must be initialised before anything of this CTA can signal them
+        cluster_arrive();
+        cluster_wait();
+    }
+    tc_fence_after();
+    const uint32_t tmem_base = tmem_base_slot;
+    pdl_launch_dependents();
+    pdl_wait();
+
+    if (warp == 0) {
+        // ---------------------------------------------------------------- producer
+        int stage = 0;
+        uint32_t phase = 0;
+        int issued = 0;
+        const bool elected = elect_one();
+        bool ok = true;  // the elected thread's
+        for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
+            int tm, tn;
+            tile_at(args, tile, &tm, &tn);
+            const int which = EPI == EPI_STORE && tn >= args.n_tiles ? 1 : 0;
+            const int m0 = tm * (CG * ROWS) + (int)rank * ROWS;
+            const int n0 = EPI == EPI_GATED ? tn * (block_n >> 1) : (tn - which * args.n_tiles) * block_n + (int)rank * own_n;
+            for (int kb = kb_begin; kb < kb_end; ++kb) {
+                const int pass = kb / args.num_kb;  // 0 or 1
+                const int k0 = (kb - pass * args.num_kb) * BK;
+                const uint32_t full = CG == 2 ? map_to_cta(smem_u32(&bar_full[stage]), 0u) : smem_u32(&bar_full[stage]);
+                const uint32_t a_dst = stage_base + (uint32_t)stage * stage_bytes, b_dst = a_dst + P * a_plane;
+                // the weights of this half of the columns, of this pass, or one and the same
+                const CUtensorMap* map_b = (EPI == EPI_GATED ? (CG == 2 && rank == 1) : pass == 1) ? &map_b1 : &map_b0;
+                if (elected && ok && (ok = bounded_wait(smem_u32(&bar_empty[stage]), phase ^ 1u, abort_flag))) {
+                    if (leader) mbar_arrive_expect_tx(smem_u32(&bar_full[stage]), tx_bytes);
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        const int pa = pass * P + p, pb = which * P + p;
+                        const uint32_t ad = a_dst + p * a_plane, bd = b_dst + p * b_plane;
+                        if (args.a_mn) {
+                            for (int i = 0; i < ROWS / 64; ++i) load3<CG>(ad + i * GROUP_BYTES, &map_a, full, m0 + 64 * i, k0, pa);
+                        } else {
+                            load3<CG>(ad, &map_a, full, k0, m0, pa);
+                        }
+                        if (EPI == EPI_GATED && CG == 1) {
+                            const int half = own_n >> 1;
+                            for (int w = 0; w < 2; ++w) {
+                                const CUtensorMap* mb = w ? &map_b1 : &map_b0;
+                                if (args.b_mn) {
+                                    for (int i = 0; i < half / 64; ++i) load3<CG>(bd + w * half * 128 + i * GROUP_BYTES, mb, full, n0 + 64 * i, k0, pb);
+                                } else {
+                                    load3<CG>(bd + w * half * 128, mb, full, k0, n0, pb);
+                                }
+                            }
+                        } else if (args.b_mn) {
+                            for (int i = 0; i < own_n / 64; ++i) load3<CG>(bd + i * GROUP_BYTES, map_b, full, n0 + 64 * i, k0, pb);
+                        } else {
+                            load3<CG>(bd, map_b, full, k0, n0, pb);
+                        }
+                    }
+                    ++issued;
+                }
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
+            }
+        }
+        if (!ok) {
+            give_up(abort_flag, args.dev_status, DEV_STATUS_TIMEOUT_PRODUCER);
+            // copies in flight must land before this CTA's shared memory goes away; the odd CTA of a pair has no barrier of
+            // its own to watch and waits out the longest that a copy can take
+            if (leader) {
+                for (int k = (issued > stages ? issued - stages : 0); k < issued; ++k)
+                    drain(smem_u32(&bar_full[k % stages]), (uint32_t)((k / stages) & 1), args.dev_status);
+            } else {
+                const unsigned long long t0 = global_ns();
+                while (global_ns() - t0 < 2000000ull) {}  // 2 ms
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------------------------------------------------------- MMA issuer (the even CTA's)
+        if (leader) {
+            const uint32_t formats = KIND == KIND_BF16 ? (1u << 4) | (1u << 7) | (1u << 10)   // fp32 sums of bfloat16
+                                                       : (2u << 4) | (1u << 7) | (1u << 10);  // 32-bit sums of signed 8-bit
+            const uint32_t idesc = formats | ((uint32_t)(block_n >> 3) << 17) | ((uint32_t)(CG * ROWS >> 4) << 24) |
+                                   (args.a_mn ? IDESC_A_MN : 0u) | (args.b_mn ? IDESC_B_MN : 0u);
+            const uint64_t a_step = args.a_mn ? 128 : 2, b_step = args.b_mn ? 128 : 2;  // of an MMA along K, in 16 bytes
+            int stage = 0;
+            uint32_t phase = 0;
+            int acc = 0;
+            uint32_t acc_phase = 0;
+            const bool elected = elect_one();
+            bool ok = true;  // the elected thread's
+            bool issued_any = false;
+            for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
+                int in_segment = 0;
+                for (int kb = kb_begin; kb < kb_end; ++kb) {
+                    if (in_segment == 0 && elected && ok) ok = bounded_wait(smem_u32(&bar_acc_empty[acc]), acc_phase ^ 1u, abort_flag);
+                    const uint32_t d = tmem_base + (uint32_t)acc * acc_cols;
+                    const uint32_t a_addr = stage_base + (uint32_t)stage * stage_bytes, b_addr = a_addr + P * a_plane;
+                    uint64_t da[P], db[P];
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        da[p] = args.a_mn ? mn_desc(a_addr + p * a_plane) : make_kmajor_sw128_desc(a_addr + p * a_plane);
+                        db[p] = args.b_mn ? mn_desc(b_addr + p * b_plane) : make_kmajor_sw128_desc(b_addr + p * b_plane);
+                    }
+                    if (elected && ok && (ok = bounded_wait(smem_u32(&bar_full[stage]), phase, abort_flag))) {
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t more = (in_segment | k) != 0 ? 1u : 0u;
+                            mma<CG, KIND>(d, da[0] + a_step * k, db[0] + b_step * k, idesc, more);
+                            if constexpr (P == 3) {
+                                const uint32_t small = d + (uint32_t)block_n;
+                                mma<CG, KIND>(small, da[2] + a_step * k, db[0] + b_step * k, idesc, more);
+                                mma<CG, KIND>(small, da[0] + a_step * k, db[2] + b_step * k, idesc, 1u);
+                                mma<CG, KIND>(small, da[1] + a_step * k, db[1] + b_step * k, idesc, 1u);
+                                mma<CG, KIND>(small, da[1] + a_step * k, db[0] + b_step * k, idesc, 1u);
+                                mma<CG, KIND>(small, da[0] + a_step * k, db[1] + b_step * k, idesc, 1u);
+                            }
+                        }
+                        commit<CG>(smem_u32(&bar_empty[stage]));
+                        issued_any = true;
+                    }
+                    if (++stage == stages) { stage = 0; phase ^= 1u; }
+                    ++in_segment;
+                    if (kb + 1 == kb_end || (P == 3 && in_segment == args.seg_kb)) {
+                        if (elected && ok) commit<CG>(smem_u32(&bar_acc_full[acc]));
+                        if (++acc == args.acc_stages) { acc = 0; acc_phase ^= 1u; }
+                        in_segment = 0;
+                    }
+                }
+            }
+            if (!ok) {
+                give_up(abort_flag, args.dev_status, DEV_STATUS_TIMEOUT_MMA);
+                if (issued_any) {  // let the MMAs already issued finish before tensor memory is released
+                    if (CG == 2) tc_commit_pair(smem_u32(&bar_drain), (uint16_t)1);
+                    else tc_commit(smem_u32(&bar_drain));
+                    drain(smem_u32(&bar_drain), 0u, args.dev_status);
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------------- epilogue (warps 2..9)
+        // Two warps for each quadrant of tensor-memory lanes (32 rows) take alternate chunks of 32 columns; a gated tile's
+        // chunks are pairs, of g and of u.
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        const int n_chunks = block_n / 32 / (EPI == EPI_GATED ? 2 : 1);  // chunks, or pairs of them
+        const int segments = P == 3 ? (kb_end - kb_begin + args.seg_kb - 1) / args.seg_kb : 1;
+        const uint32_t pitch = (uint32_t)(block_n + 4) * 4u;  // of a partial tile's row: consecutive rows start 4 banks apart
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        bool ok = true;
+        for (int tile = first_tile; ok && tile < args.num_tiles; tile += tile_step) {
+            int tm, tn;
+            tile_at(args, tile, &tm, &tn);
+            const int which = EPI == EPI_STORE && tn >= args.n_tiles ? 1 : 0;
+            const int64_t m0 = (int64_t)tm * (CG * ROWS) + (int)rank * ROWS;
+            const int n0 = EPI == EPI_GATED ? tn * (block_n >> 1) : (tn - which * args.n_tiles) * block_n;
+            float sum[P == 3 ? 2 : 1][32];  // P = 3: block_n is 128, a warp has two chunks
+            for (int segment = 0; segment < segments; ++segment) {
+                const bool got = bounded_wait(smem_u32(&bar_acc_full[acc]), acc_phase, abort_flag);
+                if (!__all_sync(0xffffffffu, got)) {
+                    if (lane == 0) give_up(abort_flag, args.dev_status, DEV_STATUS_TIMEOUT_EPILOGUE);
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t at = tmem_base + lanes + (uint32_t)acc * acc_cols;
+                const uint32_t acc_empty = CG == 2 ? map_to_cta(smem_u32(&bar_acc_empty[acc]), 0u) : smem_u32(&bar_acc_empty[acc]);
+                if constexpr (P == 3) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t large[32];
+#pragma unroll
+                        for (int part = 0; part < 2; ++part) {  // the small products first
+                            tc_ld_32x32(at + (uint32_t)((half + 2 * j) * 32 + (part ? 0 : block_n)), large);
+                            tc_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) sum[j][i] = (segment | part ? sum[j][i] : 0.f) + __uint_as_float(large[i]);
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (CG == 2) mbar_arrive_cluster(acc_empty);
+                        else mbar_arrive(acc_empty);
+                    }
+                } else if (args.splits == 1) {
+                    for (int ch = half; ch < n_chunks; ch += 2) {
+                        uint32_t first[32], up[EPI == EPI_GATED ? 32 : 1];
+                        tc_ld_32x32(at + (uint32_t)ch * 32u, first);
+                        if constexpr (EPI == EPI_GATED) tc_ld_32x32(at + (uint32_t)(block_n / 2 + ch * 32), up);
+                        tc_ld_wait();
+                        if (ch + 2 >= n_chunks) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) {
+                                if (CG == 2) mbar_arrive_cluster(acc_empty);
+                                else mbar_arrive(acc_empty);
+                            }
+                        }
+                        if constexpr (EPI == EPI_GATED) finish<P, EPI, 32>(args, which, m0 + quad * 32 + lane, n0 + ch * 32, first, up);
+                        else finish<P, EPI, 32>(args, which, m0 + quad * 32 + lane, n0 + ch * 32, first, first);
+                        __syncwarp();
+                    }
+                }
+                if (++acc == args.acc_stages) { acc = 0; acc_phase ^= 1u; }
+            }
+            if constexpr (P == 3) {
+                if (ok && args.splits == 1) {
+                    const int64_t row = m0 + quad * 32 + lane;
+                    const uint32_t(&v0)[32] = reinterpret_cast<const uint32_t(&)[32]>(sum[0]);
+                    const uint32_t(&v1)[32] = reinterpret_cast<const uint32_t(&)[32]>(sum[1]);
+                    // eight columns at a time: 128 registers are taken by the sums and what was read of them
+#pragma unroll
+                    for (int c = 0; c < 32; c += 8) {
+                        const uint32_t(&w0)[8] = reinterpret_cast<const uint32_t(&)[8]>(v0[c]);
+                        const uint32_t(&w1)[8] = reinterpret_cast<const uint32_t(&)[8]>(v1[c]);
+                        if (EPI == EPI_GATED) {
+                            finish<P, EPI, 8>(args, which, row, n0 + half * 32 + c, w0, w1);
+                        } else {
+                            finish<P, EPI, 8>(args, which, row, n0 + half * 32 + c, w0, w0);
+                            finish<P, EPI, 8>(args, which, row, n0 + (half + 2) * 32 + c, w1, w1);
+                        }
+                    }
+                }
+            }
+            if constexpr (CG == 1) {
+                if (args.splits > 1) {
+                    // every MMA of this CTA has finished, so the stages' shared memory is free for the partial tile
+                    const uint32_t row_at = stage_base + (uint32_t)(quad * 32 + lane) * pitch;
+                    if (ok && m0 + quad * 32 < args.M) {
+                        for (int j = 0; half + 2 * j < block_n / 32; ++j) {
+                            const int ch = half + 2 * j;
+                            uint32_t v[32];
+                            if constexpr (P == 3) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(j == 0 ? sum[0][i] : sum[1][i]);
+                            } else {
+                                tc_ld_32x32(tmem_base + lanes + (uint32_t)ch * 32u, v);
+                                tc_ld_wait();
+                            }
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row_at + (uint32_t)(ch * 32 + i) * 4u), "r"(v[i]),
+                                             "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]) : "memory");
+                        }
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    }
+
+    if constexpr (CG == 1) {
+        if (args.splits > 1) {
+            cluster_arrive();
+            cluster_wait();
+            // after a time-out in any CTA the sums are wrong, and the status word says so
+            if (warp >= 2) {
+                int tm, tn;
+                tile_at(args, first_tile, &tm, &tn);
+                const int which = EPI == EPI_STORE && tn >= args.n_tiles ? 1 : 0;
+                const int64_t m0 = (int64_t)tm * ROWS;
+                const int columns = EPI == EPI_GATED ? block_n >> 1 : block_n;
+                const int n0 = EPI == EPI_GATED ? tn * columns : (tn - which * args.n_tiles) * block_n;
+                const int groups = columns / 8;
+                const int rows = (int)min((int64_t)ROWS, args.M - m0);
+                const uint32_t pitch = (uint32_t)(block_n + 4) * 4u;
+                for (int item = (int)slice * 256 + (int)threadIdx.x - 64; item < rows * groups; item += 256 * args.splits) {
+                    const int row = item / groups, col = (item - row * groups) * 8;
+                    const uint32_t at = stage_base + (uint32_t)row * pitch + (uint32_t)col * 4u;
+                    uint32_t first[8], second[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) first[i] = second[i] = 0u;
+                    for (int r = 0; r < args.splits; ++r) {
+                        const uint32_t from = map_to_cta(at, (uint32_t)r);
+#pragma unroll
+                        for (int i = 0; i < 8; i += 4) {
+                            const uint4 x = lds4_cluster(from + i * 4u);
+                            add_part<KIND>(first, i, x);
+                            if (EPI == EPI_GATED) {
+                                const uint4 y = lds4_cluster(from + (uint32_t)(columns + i) * 4u);
+                                add_part<KIND>(second, i, y);
+                            }
+                        }
+                    }
+                    finish<P, EPI, 8>(args, which, m0 + row, n0 + col, first, second);
+                }
+            }
+        }
+    }
+
+    // ---------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2 || args.splits > 1) {  // nobody leaves while another may still signal or read its shared memory
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+    }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------
+
+tfjsb_status encode(tfjsb_ctx* ctx, CUtensorMap* map, const Operand& o, Kind kind, int64_t rows, int64_t K, int box_rows, const char* what) {
+    const int size = kind == KIND_BF16 ? 2 : 1, bk = 128 / size;
+    cuuint64_t dims[3] = {(cuuint64_t)(o.mn ? rows : K), (cuuint64_t)(o.mn ? K : rows), (cuuint64_t)o.planes};
+    const int64_t plane = o.planes > 1 ? o.plane : o.pitch * (o.mn ? K : rows);
+    cuuint64_t strides[2] = {(cuuint64_t)(o.pitch * size), (cuuint64_t)(plane * size)};
+    cuuint32_t box[3] = {(cuuint32_t)(o.mn ? 64 : bk), (cuuint32_t)(o.mn ? 64 : box_rows), 1u};
+    cuuint32_t elem[3] = {1u, 1u, 1u};
+    const CUresult r = ctx->encode_tiled(map, kind == KIND_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 3,
+                                         const_cast<void*>(o.base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+        return fail(ctx, TFJSB_ERR_CUDA, std::string("cuTensorMapEncodeTiled failed for ") + what + " (CUresult " + std::to_string((int)r) + ")");
+    return TFJSB_OK;
+}
+
+template <int CG, int P, int KIND, int EPI>
+cudaError_t launch(const CUtensorMap* maps, const Args& args, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
+    auto* kernel = &dense_kernel<CG, P, KIND, EPI>;
+    cudaError_t e = smem_attr_once(reinterpret_cast<const void*>(kernel), tile::SMEM_LIMIT - 2048);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    const int cluster = CG == 2 ? 2 : args.splits;
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = cluster;
+        attr[n].val.clusterDim.y = 1;
+        attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (g_launch_pdl) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    e = cudaLaunchKernelEx(&cfg, kernel, maps[0], maps[1], maps[2], args);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
+template <int CG>
+cudaError_t launch_any(const Product& p, const CUtensorMap* maps, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
+    if (p.kind == KIND_INT8) return launch<CG, 1, KIND_INT8, EPI_SCALE>(maps, p.args, grid, smem, s, launches);
+    if (p.planes == 1) {
+        if (p.epilogue == EPI_GATED) return launch<CG, 1, KIND_BF16, EPI_GATED>(maps, p.args, grid, smem, s, launches);
+        if (p.epilogue == EPI_GRAD) return launch<CG, 1, KIND_BF16, EPI_GRAD>(maps, p.args, grid, smem, s, launches);
+        return launch<CG, 1, KIND_BF16, EPI_STORE>(maps, p.args, grid, smem, s, launches);
+    }
+    if (p.epilogue == EPI_GATED) return launch<CG, 3, KIND_BF16, EPI_GATED>(maps, p.args, grid, smem, s, launches);
+    if (p.epilogue == EPI_GRAD) return launch<CG, 3, KIND_BF16, EPI_GRAD>(maps, p.args, grid, smem, s, launches);
+    return launch<CG, 3, KIND_BF16, EPI_STORE>(maps, p.args, grid, smem, s, launches);
+}
+
+// Which kernel: CTA pairs or single CTAs, columns of a tile, slices of K.
+struct Shape { int cg, block_n, splits; };
+
+int64_t tiles_of(const Product& p, int cg, int block_n) {
+    const int64_t columns = p.epilogue == EPI_GATED ? block_n / 2 : block_n;
+    return ((p.args.M + cg * ROWS - 1) / (cg * ROWS)) * ((p.args.N + columns - 1) / columns) * p.args.outputs;
+}
+
+// Estimated cycles: rounds of tiles x k-blocks x cycles of a k-block, and what a tile and a launch cost beside them.  A k-block's
+// MMAs take 2 cycles a column; single CTAs are bound by their shared memory (operand rows written and read) instead.
+double cost(const Product& p, const Shape& c, int sm_count) {
+    const int kb = (p.args.K + (p.kind == KIND_BF16 ? 63 : 127)) / (p.kind == KIND_BF16 ? 64 : 128) * p.args.passes;
+    const double per_kb = (c.cg == 2 ? 2.1 * c.block_n + 20 : 2.0 * c.block_n + 256) * (p.planes == 3 ? 6 : 1);
+    const int64_t tiles = tiles_of(p, c.cg, c.block_n);
+    const int64_t rounds = c.splits > 1 ? 1 : (tiles + sm_count / c.cg - 1) / (sm_count / c.cg);
+    const int own_kb = (kb + c.splits - 1) / c.splits;
+    return (double)rounds * own_kb * per_kb + 10.0 * c.block_n + (c.splits > 1 ? 2500 : 0) + (rounds - 1) * 200;
+}
+
+Shape choose(const Product& p, int sm_count) {
+    const char* forced = getenv("TFJSB_DENSE_SHAPE");  // "cta group,columns,slices", wherever the product allows it
+    Shape best = {1, 128, 1};
+    double least = -1;
+    const int kb = (p.args.K + (p.kind == KIND_BF16 ? 63 : 127)) / (p.kind == KIND_BF16 ? 64 : 128) * p.args.passes;
+    for (int cg = 1; cg <= 2; ++cg)
+        for (int bn = 64; bn <= 256; bn *= 2) {
+            if (p.planes == 3 && bn != 128) continue;                         // two accumulators of 128 columns, two stages
+            if (bn == 64 && (cg == 2 || p.epilogue == EPI_GATED)) continue;   // boxes are 64 columns wide
+            const int64_t tiles = tiles_of(p, cg, bn);
+            for (int splits = 1; splits <= (cg == 1 && bn <= 128 ? 8 : 1); splits *= 2) {
+                // at least four k-blocks a slice, none without any, one wave
+                const int each = (kb + splits - 1) / splits;
+                if (splits > 1 && (each < 4 || each * (splits - 1) >= kb || tiles * splits > sm_count)) continue;
+                const Shape c = {cg, bn, splits};
+                if (forced) {
+                    int f[3];
+                    if (sscanf(forced, "%d,%d,%d", &f[0], &f[1], &f[2]) == 3 && f[0] == cg && f[1] == bn && f[2] == splits) return c;
+                }
+                const double cycles = cost(p, c, sm_count);
+                if (least < 0 || cycles < least) { least = cycles; best = c; }
+            }
+        }
+    return best;
+}
+
+}  // namespace
+
+tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
+    if (!ctx->encode_tiled) return fail(ctx, TFJSB_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+    Args& a = p.args;
+    const Shape c = choose(p, ctx->sm_count);
+    const int bk = p.kind == KIND_BF16 ? 64 : 128;
+    a.block_n = c.block_n;
+    a.splits = c.splits;
+    a.acc_stages = 2;
+    a.seg_kb = 2;  // 8 additions to an accumulator of large products
+    a.num_kb = (a.K + bk - 1) / bk;
+    a.kb_per_split = (a.num_kb * a.passes + c.splits - 1) / c.splits;
+    a.m_tiles = (a.M + c.cg * ROWS - 1) / (c.cg * ROWS);
+    const int columns = p.epilogue == EPI_GATED ? c.block_n / 2 : c.block_n;
+    a.n_tiles = (a.N + columns - 1) / columns;
+    const int64_t tiles = tiles_of(p, c.cg, c.block_n);
+    if (tiles >= (1LL << 31)) return fail(ctx, TFJSB_ERR_UNSUPPORTED, "too many tiles");
+    a.num_tiles = (int)tiles;
+    a.a_mn = p.a.mn;
+    a.b_mn = p.b[0].mn;
+    // of a matrix of less rows than a tile only those are copied (a multiple of 8, the swizzle's period): the others' sums are not stored
+    a.a_rows = !p.a.mn && a.M < ROWS ? (a.M + 7) / 8 * 8 : ROWS;
+    a.dev_status = ctx->dev_status;
+    const int own_n = c.block_n / c.cg;
+    const int stage_bytes = p.planes * (A_BYTES + own_n * 128);
+    int stages = (tile::SMEM_LIMIT - 2048 - 1024) / stage_bytes;
+    a.stages = stages < MAX_STAGES ? stages : MAX_STAGES;
+    const size_t smem = 1024 + (size_t)a.stages * stage_bytes;
+    CUtensorMap maps[3];
+    tfjsb_status st;
+    const int b_rows = p.epilogue == EPI_GATED ? c.block_n / 2 : own_n;
+    if ((st = encode(ctx, &maps[0], p.a, p.kind, a.M, a.K, a.a_rows, "A")) != TFJSB_OK) return st;
+    if ((st = encode(ctx, &maps[1], p.b[0], p.kind, a.N, a.K, b_rows, "B")) != TFJSB_OK) return st;
+    if (p.b[1].base) {
+        if ((st = encode(ctx, &maps[2], p.b[1], p.kind, a.N, a.K, b_rows, "B")) != TFJSB_OK) return st;
+    } else {
+        maps[2] = maps[1];
+    }
+    const int64_t slots = ctx->sm_count / c.cg;
+    const int grid = (int)(c.splits > 1 ? tiles * c.splits : (tiles < slots ? tiles : slots) * c.cg);
+    const cudaError_t e = c.cg == 2 ? launch_any<2>(p, maps, grid, smem, s, &ctx->launches) : launch_any<1>(p, maps, grid, smem, s, &ctx->launches);
+    return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "dense product launch");
+}
+
+}  // namespace dense
+}  // namespace tfjsb

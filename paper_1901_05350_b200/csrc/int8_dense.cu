@@ -1,0 +1,263 @@
+// Dense layers on 8-bit integers: rows quantised with a scale of their own, products with exact 32-bit sums (dense_tcgen05.cu, kind::i8), and
+// the epilogue act(sum a_scale b_scale + bias).
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+#include "dense.cuh"
+#include "dense_math.cuh"
+#include "ptx_sm100.cuh"
+
+namespace tfjsb {
+namespace dense {
+namespace {
+
+constexpr int64_t MAX_K = 131072;  // 2^17 products of at most 2^14: sums fit 32 bits
+constexpr int QUANTIZE_THREADS = 256;
+
+// ---- quantising a row ---------------------------------------------------------------------------------------
+// q = 127 x / amax rounded to nearest, halves to even.  Whether a value lies above, on or below the middle between two integers is decided
+// exactly: 127 |x| is t + t_low (a product and its fma rest), q0 the integer nearest to t / amax as computed, and the sign of
+// 127 |x| - (q0 +- 1/2) amax, of which t - q0 amax is exact (one fma; the terms nearly cancel), settles whether q0 is it.
+// Rows of very small or large values are scaled by a power of two first, so that nothing here overflows or loses bits.
+struct RowScale {
+    float pre, amax, inverse;  // of pre * x
+    bool none;                 // q = 0: amax is 0, infinite or NaN
+};
+__device__ __forceinline__ RowScale row_scale(float amax) {
+    RowScale r;
+    r.none = !(amax > 0.f) || !isfinite(amax);
+    r.pre = amax < 7.8886091e-31f ? 1.2676506e30f : amax > 1.2676506e30f ? 7.8886091e-31f : 1.f;  // 2^-100, 2^100
+    r.amax = amax * r.pre;
+    r.inverse = 1.f / r.amax;
+    return r;
+}
+__device__ __forceinline__ int quantize(float x, const RowScale& r) {
+    if (r.none) return 0;
+    const float v = fabsf(x * r.pre);
+    const float t = v * 127.f, t_low = fmaf(v, 127.f, -t);
+    float q = rintf(t * r.inverse);
+    const float e = fmaf(-q, r.amax, t), middle = 0.5f * r.amax;
+    const bool odd = ((int)q & 1) != 0;
+    const float above = (e - middle) + t_low, below = (e + middle) + t_low;
+    if (above > 0.f || (above == 0.f && odd)) q += 1.f;
+    else if (below < 0.f || (below == 0.f && odd)) q -= 1.f;
+    return x < 0.f ? -(int)q : (int)q;
+}
+// The larger of two magnitudes; a NaN wins over all.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+template <bool F32>
+__device__ __forceinline__ float value_at(const void* x, int64_t i) {
+    if (F32) return load_global(static_cast<const float*>(x) + i);
+    return __uint_as_float((uint32_t)load_global(static_cast<const unsigned short*>(x) + i) << 16);
+}
+// Eight values from element i on, of which `left` exist.
+template <bool F32>
+__device__ __forceinline__ void values8(const void* x, int64_t i, int left, float (&v)[8]) {
+    if (F32) {
+        load_f32(static_cast<const float*>(x) + i, v, left);
+        return;
+    }
+    const unsigned short* p = static_cast<const unsigned short*>(x) + i;
+    if (left >= 8 && aligned(p, 16)) {
+        uint32_t w[4];
+        asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __uint_as_float(w[e] << 16);
+            v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? __uint_as_float((uint32_t)load_global(p + e) << 16) : 0.f;
+    }
+}
+
+// A block has a row: its values stay in registers between the maximum and the rounding, up to 4 groups of eight a thread; those
+// of longer rows are read again.
+template <bool F32>
+__global__ void __launch_bounds__(QUANTIZE_THREADS) quantize_kernel(const void* x, int64_t columns, int64_t pitch, int8_t* q, float* scale) {
+    ptx::pdl_launch_dependents();
+    ptx::pdl_wait();
+    __shared__ float part[QUANTIZE_THREADS / 32];
+    constexpr int HELD = 4, STEP = QUANTIZE_THREADS * 8;
+    const int64_t row = blockIdx.x;
+    const int64_t base = row * columns;
+    float held[HELD][8];
+    float amax = 0.f;
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) {
+        const int64_t c = (int64_t)j * STEP + threadIdx.x * 8;
+        if (c < columns) {
+            values8<F32>(x, base + c, columns - c < 8 ? (int)(columns - c) : 8, held[j]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) amax = max_nan(amax, fabsf(held[j][e]));
+        }
+    }
+    for (int64_t c = (int64_t)HELD * STEP + threadIdx.x * 8; c < columns; c += STEP) {
+        float v[8];
+        values8<F32>(x, base + c, columns - c < 8 ? (int)(columns - c) : 8, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax = max_nan(amax, fabsf(v[e]));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = amax;
+    __syncthreads();
+    amax = part[0];
+#pragma unroll
+    for (int w = 1; w < QUANTIZE_THREADS / 32; ++w) amax = max_nan(amax, part[w]);
+    const RowScale r = row_scale(amax);
+    if (threadIdx.x == 0) scale[row] = amax / 127.f;
+#pragma unroll 1
+    for (int j = 0; j * (int64_t)STEP < pitch; ++j) {
+        const int64_t c = (int64_t)j * STEP + threadIdx.x * 8;
+        if (c >= pitch) break;
+        float v[8];
+        if (j < HELD && c < columns) {
+#pragma unroll
+            for (int k = 0; k < HELD; ++k)
+                if (k == j) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = held[k][e];
+                }
+        } else if (c < columns) {
+            values8<F32>(x, base + c, columns - c < 8 ? (int)(columns - c) : 8, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = 0.f;
+        }
+        uint32_t w[2] = {0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e / 4] |= (uint32_t)(quantize(v[e], r) & 0xff) << (e % 4 * 8);
+        *reinterpret_cast<uint2*>(q + row * pitch + c) = make_uint2(w[0], w[1]);  // the pitch is a multiple of 16
+    }
+}
+
+cudaError_t launch_quantize(bool f32, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, cudaStream_t s, int64_t* launches) {
+    const int64_t pitch = (columns + 15) / 16 * 16;
+    const cudaError_t e = f32 ? launch_k(quantize_kernel<true>, dim3((unsigned)rows), dim3(QUANTIZE_THREADS), 0, s, x, columns, pitch, q, scale)
+                              : launch_k(quantize_kernel<false>, dim3((unsigned)rows), dim3(QUANTIZE_THREADS), 0, s, x, columns, pitch, q, scale);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
+bool known(tfjsb_dtype d) { return d == TFJSB_DTYPE_F32 || d == TFJSB_DTYPE_BF16; }
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+    if (!a || !b || a_bytes <= 0 || b_bytes <= 0) return false;
+    const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
+int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
+
+tfjsb_status check_product(tfjsb_ctx* ctx, const void* bt, const float* b_scale, const float* bias, tfjsb_act act, void* out, tfjsb_dtype out_dtype,
+                           int64_t M, int64_t N, int64_t K) {
+    if (!known(out_dtype)) return fail(ctx, TFJSB_ERR_INVALID_ARG, "unknown dtype");
+    if (act != TFJSB_ACT_NONE && act != TFJSB_ACT_RELU && act != TFJSB_ACT_RELU6) return fail(ctx, TFJSB_ERR_INVALID_ARG, "unknown activation");
+    if (M < 0 || N < 0 || K < 1 || M > (1LL << 30) || N > (1LL << 30)) return fail(ctx, TFJSB_ERR_SHAPE, "sizes: 0 <= M, N <= 2^30, K >= 1");
+    if (K > MAX_K) return fail(ctx, TFJSB_ERR_UNSUPPORTED, "K is above 131072: 32-bit sums could overflow");
+    if (M == 0 || N == 0) return TFJSB_OK;
+    if (!bt || !b_scale || !out) return fail(ctx, TFJSB_ERR_INVALID_ARG, "bt / b_scale / out is null");
+    if (!aligned(bt, 16) || !aligned(out, 16) || !aligned(b_scale, 16) || (bias && !aligned(bias, 16)))
+        return fail(ctx, TFJSB_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    const int64_t bytes = M * N * (out_dtype == TFJSB_DTYPE_F32 ? 4 : 2);
+    if (overlap(out, bytes, bt, N * up16(K)) || overlap(out, bytes, b_scale, 4 * N) || overlap(out, bytes, bias, 4 * N))
+        return fail(ctx, TFJSB_ERR_INVALID_ARG, "out overlaps an input");
+    return TFJSB_OK;
+}
+
+tfjsb_status product(tfjsb_ctx* ctx, const int8_t* a, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias, tfjsb_act act,
+                     void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, cudaStream_t s) {
+    Product p;
+    p.kind = KIND_INT8;
+    p.epilogue = EPI_SCALE;
+    p.a.base = a;
+    p.a.pitch = K;
+    p.b[0].base = bt;
+    p.b[0].pitch = K;
+    p.args.M = (int)M; p.args.N = (int)N; p.args.K = (int)K;
+    p.args.out[0] = out;
+    p.args.out_pitch = N;
+    p.args.out_bf16 = out_dtype == TFJSB_DTYPE_BF16;
+    p.args.act = act;
+    p.args.a_scale = a_scale;
+    p.args.b_scale = b_scale;
+    p.args.bias = bias;
+    return run_product(ctx, p, s);
+}
+
+}  // namespace
+}  // namespace dense
+}  // namespace tfjsb
+
+using namespace tfjsb;
+using namespace tfjsb::dense;
+
+extern "C" {
+
+tfjsb_status tfjsb_quantize_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, void* stream) {
+    if (!ctx) return TFJSB_ERR_INVALID_ARG;
+    const dense::OnDevice on(ctx);
+    if (!known(dtype)) return fail(ctx, TFJSB_ERR_INVALID_ARG, "unknown dtype");
+    if (rows < 0 || rows > (1LL << 30) || columns < 1) return fail(ctx, TFJSB_ERR_SHAPE, "sizes: 0 <= rows <= 2^30, columns >= 1");
+    if (columns > MAX_K) return fail(ctx, TFJSB_ERR_UNSUPPORTED, "more than 131072 columns");
+    if (rows == 0) return TFJSB_OK;
+    if (!x || !q || !scale) return fail(ctx, TFJSB_ERR_INVALID_ARG, "x / q / scale is null");
+    if (!aligned(x, 16) || !aligned(q, 16) || !aligned(scale, 16)) return fail(ctx, TFJSB_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    const int64_t in = rows * columns * (dtype == TFJSB_DTYPE_F32 ? 4 : 2), out = rows * up16(columns);
+    if (overlap(x, in, q, out) || overlap(x, in, scale, 4 * rows) || overlap(q, out, scale, 4 * rows))
+        return fail(ctx, TFJSB_ERR_INVALID_ARG, "x, q and scale overlap");
+    const cudaError_t e = launch_quantize(dtype == TFJSB_DTYPE_F32, x, rows, columns, q, scale, static_cast<cudaStream_t>(stream), &ctx->launches);
+    return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "quantize launch");
+}
+
+tfjsb_status tfjsb_matmul_int8(tfjsb_ctx* ctx, const int8_t* a, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias,
+                               tfjsb_act act, void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, void* stream) {
+    if (!ctx) return TFJSB_ERR_INVALID_ARG;
+    const dense::OnDevice on(ctx);
+    const tfjsb_status st = check_product(ctx, bt, b_scale, bias, act, out, out_dtype, M, N, K);
+    if (st != TFJSB_OK) return st;
+    if (K % 16) return fail(ctx, TFJSB_ERR_UNSUPPORTED, "K must be a multiple of 16: fill rows up with zeros");
+    if (M == 0 || N == 0) return TFJSB_OK;
+    if (!a || !a_scale) return fail(ctx, TFJSB_ERR_INVALID_ARG, "a / a_scale is null");
+    if (!aligned(a, 16) || !aligned(a_scale, 16)) return fail(ctx, TFJSB_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    const int64_t bytes = M * N * (out_dtype == TFJSB_DTYPE_F32 ? 4 : 2);
+    if (overlap(out, bytes, a, M * K) || overlap(out, bytes, a_scale, 4 * M)) return fail(ctx, TFJSB_ERR_INVALID_ARG, "out overlaps an input");
+    return product(ctx, a, a_scale, bt, b_scale, bias, act, out, out_dtype, M, N, K, static_cast<cudaStream_t>(stream));
+}
+
+int64_t tfjsb_dense_int8_workspace(int64_t M, int64_t K) {
+    if (M < 0 || K < 1 || M > (1LL << 30) || K > MAX_K) return 0;
+    return up256(M * up16(K)) + up256(4 * M);
+}
+
+tfjsb_status tfjsb_dense_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, const int8_t* bt, const float* b_scale, const float* bias, tfjsb_act act,
+                              void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, void* workspace, int64_t workspace_bytes, void* stream) {
+    if (!ctx) return TFJSB_ERR_INVALID_ARG;
+    const dense::OnDevice on(ctx);
+    if (!known(dtype)) return fail(ctx, TFJSB_ERR_INVALID_ARG, "unknown dtype");
+    const tfjsb_status st = check_product(ctx, bt, b_scale, bias, act, out, out_dtype, M, N, K);
+    if (st != TFJSB_OK) return st;
+    if (M == 0 || N == 0) return TFJSB_OK;
+    const int64_t needed = tfjsb_dense_int8_workspace(M, K);
+    if (workspace_bytes < needed) return fail(ctx, TFJSB_ERR_INVALID_ARG, "the workspace needs " + std::to_string(needed) + " bytes");
+    if (!x || !workspace) return fail(ctx, TFJSB_ERR_INVALID_ARG, "x / workspace is null");
+    if (!aligned(x, 16) || !aligned(workspace, 16)) return fail(ctx, TFJSB_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    const int64_t x_bytes = M * K * (dtype == TFJSB_DTYPE_F32 ? 4 : 2), out_bytes = M * N * (out_dtype == TFJSB_DTYPE_F32 ? 4 : 2);
+    if (overlap(out, out_bytes, x, x_bytes) || overlap(out, out_bytes, workspace, needed) || overlap(workspace, needed, x, x_bytes) ||
+        overlap(workspace, needed, bt, N * up16(K)) || overlap(workspace, needed, b_scale, 4 * N) || overlap(workspace, needed, bias, 4 * N))
+        return fail(ctx, TFJSB_ERR_INVALID_ARG, "out or the workspace overlaps another argument");
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int8_t* q = static_cast<int8_t*>(workspace);
+    float* scale = reinterpret_cast<float*>(q + up256(M * up16(K)));
+    const cudaError_t e = launch_quantize(dtype == TFJSB_DTYPE_F32, x, M, K, q, scale, s, &ctx->launches);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "quantize launch");
+    return product(ctx, q, scale, bt, b_scale, bias, act, out, out_dtype, M, N, up16(K), s);
+}
+
+}  // extern "C"
