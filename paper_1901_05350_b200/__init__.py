@@ -513,10 +513,9 @@ class Context:
         """y = (gate(x w_gate) * (x w_up)) w_down: x [..., width], w_gate and w_up [width, hidden], w_down [hidden, out_width], all bfloat16
         or all fp32; gate one of silu, gelu, gelu_tanh, sigmoid, relu.  With `save`, returns (y, h, z): what gated_ffn_backprop
         needs besides its inputs (opaque)."""
-        if not save:
-            done = _fast.gated_ffn(self._fh, self.device, x, w_gate, w_up, w_down, GATE.get(gate, -1), out)
-            if done is not None:
-                return done
+        done = _fast.gated_ffn(self._fh, self.device, x, w_gate, w_up, w_down, GATE.get(gate, -1), save, out)
+        if done is not None:
+            return done
         f, sizes = self._ffn(x, w_gate, w_up, w_down, gate)
         shape = tuple(x.shape[:-1]) + (f.out_width,)
         y = self._new(shape, x.dtype) if out is None else _plain(out, "out", x.dtype, shape, self.device)
@@ -529,6 +528,10 @@ class Context:
 
     def gated_ffn_backprop(self, x, w_gate, w_up, w_down, h, z, dy, gate: str = "silu", want=(True, True, True, True)):
         """(dx, dw_gate, dw_up, dw_down) of gated_ffn, given what it saved and the gradient of y; None for those not in `want`."""
+        if all(want):
+            done = _fast.gated_ffn_backprop(self._fh, self.device, x, w_gate, w_up, w_down, h, z, dy, GATE.get(gate, -1))
+            if done is not None:
+                return done
         import torch
 
         f, sizes = self._ffn(x, w_gate, w_up, w_down, gate)

@@ -25,7 +25,7 @@ namespace {
     X(tfjsb_binary) X(tfjsb_softmax) X(tfjsb_bias_act) X(tfjsb_conv2d_backprop_input) X(tfjsb_conv2d_backprop_filter)         \
     X(tfjsb_depthwise_conv2d_backprop_input) X(tfjsb_depthwise_conv2d_backprop_filter) X(tfjsb_act_backprop)                  \
     X(tfjsb_bias_backprop) X(tfjsb_run_model) X(tfjsb_model_layer_output_f32) X(tfjsb_model_layer_shape) X(tfjsb_window_out_shape)       \
-    X(tfjsb_last_error) X(tfjsb_gated_ffn_sizes) X(tfjsb_gated_ffn) X(tfjsb_dropout) X(tfjsb_dense_int8_workspace) X(tfjsb_dense_int8)
+    X(tfjsb_last_error) X(tfjsb_gated_ffn_sizes) X(tfjsb_gated_ffn) X(tfjsb_gated_ffn_backprop) X(tfjsb_dropout) X(tfjsb_dense_int8_workspace) X(tfjsb_dense_int8)
 #define DECLARE(name) decltype(&::name) p_##name = nullptr;
 FAST_CALLS(DECLARE)
 #undef DECLARE
@@ -429,35 +429,95 @@ struct DenseOut {
     }
 };
 
-// gated_ffn(ctx, device, x, w_gate, w_up, w_down, gate, out)
+// x, w_gate, w_up, w_down and the gate of a gated feed-forward call.
+struct FfnArgs {
+    const at::Tensor* t[4];
+    int dtype = -1;
+    tfjsb_ffn f{};
+    int64_t h_bytes = 0, z_bytes = 0, work_bytes = 0, grad_work_bytes = 0;
+    int64_t y_shape[8];
+
+    at::IntArrayRef y() const { return at::IntArrayRef(y_shape, t[0]->dim()); }
+    bool take(Args& a, int device) {  // the tensors
+        for (auto& p : t) {
+            p = dense_tensor(a, device, &dtype);
+            if (!p) return false;
+        }
+        return true;
+    }
+    bool shapes(int gate) {
+        const at::Tensor& x = *t[0];
+        if (x.dim() < 1 || x.dim() > 8 || t[1]->dim() != 2 || t[3]->dim() != 2) return false;
+        const int64_t width = x.size(-1), hidden = t[1]->size(1), out_width = t[3]->size(1);
+        if (width < 1 || !has_shape(*t[1], width, hidden) || !has_shape(*t[2], width, hidden) || !has_shape(*t[3], hidden, out_width)) return false;
+        f = {x.numel() / width, width, hidden, out_width, dtype, gate};
+        for (int64_t i = 0; i < x.dim(); ++i) y_shape[i] = x.size(i);
+        y_shape[x.dim() - 1] = out_width;
+        return f.tokens > 0 && p_tfjsb_gated_ffn_sizes(&f, &h_bytes, &z_bytes, &work_bytes, &grad_work_bytes) == TFJSB_OK;
+    }
+    const void* data(int i) const { return t[i]->const_data_ptr(); }
+};
+void* writable(const at::TensorBase& t) { return const_cast<void*>(t.const_data_ptr()); }
+
+// gated_ffn(ctx, device, x, w_gate, w_up, w_down, gate, save, out): y, or (y, h, z)
 PyObject* gated_ffn(Args& a) {
     const Head h(a);
-    int dtype = -1;
-    const at::Tensor* t[4];
-    for (auto& p : t) {
-        p = dense_tensor(a, h.device, &dtype);
-        if (!p) Py_RETURN_NONE;
-    }
-    const int gate = (int)a.integer();
-    const at::Tensor& x = *t[0];
-    if (!a.ok || x.dim() < 1 || x.dim() > 8 || t[1]->dim() != 2 || t[3]->dim() != 2) Py_RETURN_NONE;
-    const int64_t width = x.size(-1), hidden = t[1]->size(1), out_width = t[3]->size(1);
-    if (width < 1 || !has_shape(*t[1], width, hidden) || !has_shape(*t[2], width, hidden) || !has_shape(*t[3], hidden, out_width)) Py_RETURN_NONE;
-    const tfjsb_ffn f = {x.numel() / width, width, hidden, out_width, dtype, gate};
-    int64_t bytes = 0;
-    if (f.tokens < 1 || p_tfjsb_gated_ffn_sizes(&f, nullptr, nullptr, &bytes, nullptr) != TFJSB_OK) Py_RETURN_NONE;
-    int64_t shape[8];
-    for (int64_t i = 0; i < x.dim(); ++i) shape[i] = x.size(i);
-    shape[x.dim() - 1] = out_width;
+    FfnArgs in;
+    if (!in.take(a, h.device)) Py_RETURN_NONE;
+    const int gate = (int)a.integer(), save = (int)a.integer();
+    if (!a.ok || !in.shapes(gate)) Py_RETURN_NONE;
     DenseOut out;
-    out.take(a, h.device, at::IntArrayRef(shape, x.dim()), &dtype);
+    out.take(a, h.device, in.y(), &in.dtype);
     if (!a.ok) Py_RETURN_NONE;
-    const at::TensorBase work = new_tensor({bytes}, at::kByte, h.device);
+    at::TensorBase kept[2];
+    if (save) {
+        kept[0] = new_tensor({in.h_bytes}, at::kByte, h.device);
+        kept[1] = new_tensor({in.z_bytes}, at::kByte, h.device);
+    }
+    const at::TensorBase work = new_tensor({in.work_bytes}, at::kByte, h.device);
     void* s = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)h.device).stream();
-    return out.done(h.ctx, unlocked([&] {
-        return p_tfjsb_gated_ffn(h.ctx, &f, x.const_data_ptr(), t[1]->const_data_ptr(), t[2]->const_data_ptr(), t[3]->const_data_ptr(), out.data, nullptr,
-                                 nullptr, const_cast<void*>(work.const_data_ptr()), bytes, s);
-    }));
+    const tfjsb_status st = unlocked([&] {
+        return p_tfjsb_gated_ffn(h.ctx, &in.f, in.data(0), in.data(1), in.data(2), in.data(3), out.data, save ? writable(kept[0]) : nullptr,
+                                 save ? writable(kept[1]) : nullptr, writable(work), in.work_bytes, s);
+    });
+    PyObject* y = out.done(h.ctx, st);
+    if (!y || !save) return y;
+    PyObject* all = PyTuple_New(3);
+    if (!all) { Py_DECREF(y); return nullptr; }
+    PyTuple_SET_ITEM(all, 0, y);
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(all, 1 + i, THPVariable_Wrap(std::move(kept[i])));
+    return all;
+}
+
+// gated_ffn_backprop(ctx, device, x, w_gate, w_up, w_down, h, z, dy, gate): the four gradients
+PyObject* gated_ffn_backprop(Args& a) {
+    const Head h(a);
+    FfnArgs in;
+    if (!in.take(a, h.device)) Py_RETURN_NONE;
+    const at::Tensor* kept[2];
+    for (auto& p : kept) {
+        PyObject* o = a.next();
+        if (!o || !THPVariable_Check(o)) Py_RETURN_NONE;
+        p = &THPVariable_Unpack(o);
+        if (p->scalar_type() != at::kByte || !p->is_cuda() || p->get_device() != h.device || !p->is_contiguous()) Py_RETURN_NONE;
+    }
+    const at::Tensor* dy = dense_tensor(a, h.device, &in.dtype);
+    const int gate = (int)a.integer();
+    if (!a.ok || !in.shapes(gate) || dy->sizes() != in.y() || kept[0]->numel() != in.h_bytes || kept[1]->numel() != in.z_bytes) Py_RETURN_NONE;
+    at::TensorBase grads[4];
+    for (int i = 0; i < 4; ++i) grads[i] = new_tensor(in.t[i]->sizes(), scalar_of(in.dtype), h.device);
+    const at::TensorBase work = new_tensor({in.grad_work_bytes}, at::kByte, h.device);
+    void* s = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)h.device).stream();
+    const tfjsb_status st = unlocked([&] {
+        return p_tfjsb_gated_ffn_backprop(h.ctx, &in.f, in.data(0), in.data(1), in.data(2), in.data(3), kept[0]->const_data_ptr(), kept[1]->const_data_ptr(),
+                                          dy->const_data_ptr(), writable(grads[0]), writable(grads[1]), writable(grads[2]), writable(grads[3]),
+                                          writable(work), in.grad_work_bytes, s);
+    });
+    if (st != TFJSB_OK) return Out().done(h.ctx, st);
+    PyObject* all = PyTuple_New(4);
+    if (!all) return nullptr;
+    for (int i = 0; i < 4; ++i) PyTuple_SET_ITEM(all, i, THPVariable_Wrap(std::move(grads[i])));
+    return all;
 }
 
 // dropout(ctx, device, x, rate, seed, offset, noise shape or None, residual or None, out)
@@ -545,7 +605,8 @@ PyMethodDef methods[] = {
     METHOD("bias_backprop", bias_backprop, 4),
     METHOD("run_model", run_model, 6),
     METHOD("layer_output_f32", layer_output_f32, 4),
-    METHOD("gated_ffn", gated_ffn, 8),
+    METHOD("gated_ffn", gated_ffn, 9),
+    METHOD("gated_ffn_backprop", gated_ffn_backprop, 10),
     METHOD("dropout", dropout, 9),
     METHOD("dense_int8", dense_int8, 9),
     {nullptr, nullptr, 0, nullptr},

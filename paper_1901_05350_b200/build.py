@@ -41,6 +41,7 @@ SOURCES = [
     "gemm_strided_tcgen05.cu",
     "chain_cluster.cu",
     "dense_tcgen05.cu",
+    "few_rows.cu",
     "gated_ffn.cu",
     "dropout.cu",
     "int8_dense.cu",

@@ -29,8 +29,8 @@ struct Operand {
 
 struct Args {
     int M = 0, N = 0, K = 0;      // of one pass; N: columns of one output (of h for EPI_GATED)
-    int block_n = 0, stages = 0, acc_stages = 0;
-    int n_tiles = 0, m_tiles = 0, outputs = 1, num_tiles = 0, band = 8;
+    int block_n = 0, stages = 0;
+    int n_tiles = 0, m_tiles = 0, outputs = 1, num_tiles = 0, whole_tiles = 0, band = 8;
     int passes = 1, num_kb = 0, kb_per_split = 0, seg_kb = 0;
     int splits = 1;
     int a_mn = 0, b_mn = 0, a_rows = 0;
@@ -54,6 +54,20 @@ struct Product {
     Args args;
 };
 tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s);
+
+// Products of few rows (few_rows.cu).  h is fp32 [rows, N]; operands 16-byte aligned, of any sizes.
+constexpr int FEW_ROWS = 8;
+tfjsb_status few_rows_gated(tfjsb_ctx* ctx, bool f32, const void* x, const void* w_gate, const void* w_up, int gate, float* h, int64_t rows, int64_t N,
+                            int64_t K, cudaStream_t s);
+tfjsb_status few_rows_down(tfjsb_ctx* ctx, bool f32, const float* h, const void* w, void* y, int64_t rows, int64_t N, int64_t K, cudaStream_t s);
+// x_kind: 0 8-bit values [rows, K rounded up to 16] with a_scale, 1 bfloat16, 2 fp32.  The rows' 8-bit values have to fit shared memory.
+constexpr int FEW_INT8_BYTES = 98304;
+inline bool few_rows_int8_supported(int64_t rows, int64_t K) {
+    const int64_t held = rows <= 2 ? rows : rows <= 4 ? 4 : 8;
+    return rows <= FEW_ROWS && held * ((K + 15) / 16 * 16) <= FEW_INT8_BYTES;
+}
+tfjsb_status few_rows_int8(tfjsb_ctx* ctx, int x_kind, const void* x, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias,
+                           int act, void* out, bool out_bf16, int64_t rows, int64_t N, int64_t K, cudaStream_t s);
 
 // The context's device is the current one while this lives: tensors say where they are, the caller's device may be another.
 struct OnDevice {

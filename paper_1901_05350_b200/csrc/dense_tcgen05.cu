@@ -93,6 +93,9 @@ __device__ __forceinline__ uint4 lds4_cluster(uint32_t addr) {
     return v;
 }
 
+__device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[32]) { tc_ld_32x32(at, r); }
+__device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[16]) { tc_ld_cols(at, r); }
+
 // Tile number -> (tile row, tile column), in bands of `band` tile rows, down a band's columns one after the other.
 __device__ __forceinline__ void tile_at(const Args& a, int tile, int* m, int* n) {
     const int columns = a.n_tiles * a.outputs;
@@ -103,8 +106,41 @@ __device__ __forceinline__ void tile_at(const Args& a, int tile, int* m, int* n)
     *m = b * a.band + in - *n * rows;
 }
 
+// A work item: a tile, and the first and the number of its 256-row parts (SUBS = 2).
+struct Item {
+    int tm, tn, sub, subs;
+};
+template <int SUBS>
+__device__ __forceinline__ Item item_at(const Args& a, int item) {
+    Item it;
+    if (SUBS == 1) {
+        tile_at(a, item, &it.tm, &it.tn);
+        it.sub = 0;
+        it.subs = 1;
+        return it;
+    }
+    const bool whole = item < a.whole_tiles;
+    tile_at(a, whole ? item : a.whole_tiles + ((item - a.whole_tiles) >> 1), &it.tm, &it.tn);
+    it.sub = whole ? 0 : (item - a.whole_tiles) & 1;
+    it.subs = whole && (int64_t)it.tm * (2 * SUBS * ROWS) + 2 * ROWS < a.M ? 2 : 1;
+    return it;
+}
+
 // ---- what becomes of W sums of a row -------------------------------------------------------------------
-// `first` and, for EPI_GATED, `second` are the sums (g and u) of columns col .. col + W - 1 of row `row`; W is 8 or 32.
+// `first` and, for EPI_GATED, `second` are the sums (g and u) of columns col .. col + W - 1 of row `row`; W is 8, 16 or 32.
+template <int P, int W>
+__device__ __forceinline__ void finish_gradient(const Args& a, int64_t row, int col, const uint32_t (&first)[W], const float (&g)[W], const float (&u)[W]) {
+    const int left = a.N - col;
+    if (row >= a.M || left <= 0) return;
+    float v[W], du[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = __uint_as_float(first[i]);
+    gated_gradient<P == 3>(a.gate, g, u, v, du);  // v: dh -> dg
+    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out[0]) + row * a.out_pitch + col;
+    store_planes<P>(dst, a.out_plane, v, left);
+    store_planes<P>(dst + P * a.out_plane, a.out_plane, du, left);
+}
+
 template <int P, int EPI, int W>
 __device__ __forceinline__ void finish(const Args& a, int which, int64_t row, int col, const uint32_t (&first)[W], const uint32_t (&second)[W]) {
     const int left = a.N - col;  // columns that exist
@@ -141,20 +177,15 @@ __device__ __forceinline__ void finish(const Args& a, int which, int64_t row, in
         gated<P == 3>(a.gate, g, u, v);
         store_planes<P>(static_cast<__nv_bfloat16*>(a.out[0]) + row * a.out_pitch + col, a.out_plane, v, left);
     } else {
-        float g[W], u[W], du[W];
+        float g[W], u[W];
         const float* z = a.z + row * a.z_pitch + col;
         load_f32(z, g, left);
         load_f32(z + (int64_t)a.M * a.z_pitch, u, left);
-#pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = __uint_as_float(first[i]);
-        gated_gradient<P == 3>(a.gate, g, u, v, du);  // v: dh -> dg
-        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out[0]) + row * a.out_pitch + col;
-        store_planes<P>(dst, a.out_plane, v, left);
-        store_planes<P>(dst + P * a.out_plane, a.out_plane, du, left);
+        finish_gradient<P, W>(a, row, col, first, g, u);
     }
 }
 
-template <int CG, int P, int KIND, int EPI>
+template <int CG, int P, int KIND, int EPI, int SUBS>
 __global__ void __launch_bounds__(THREADS, 1)
 dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1,
              const __grid_constant__ Args args) {
@@ -175,8 +206,9 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const int block_n = args.block_n, stages = args.stages;
     const int own_n = block_n / CG;  // columns of B that this CTA fetches
     const uint32_t a_plane = A_BYTES, b_plane = (uint32_t)own_n * 128u;
-    const uint32_t stage_bytes = P * (a_plane + b_plane);
-    const uint32_t tx_bytes = CG * P * ((uint32_t)args.a_rows * 128u + b_plane);
+    constexpr int TILE_M = CG * ROWS * SUBS;
+    const uint32_t stage_bytes = SUBS * P * a_plane + P * b_plane;
+    const uint32_t a_tx = CG * P * (uint32_t)args.a_rows * 128u, b_tx = CG * P * b_plane;
     const int first_tile = args.splits > 1 ? (int)blockIdx.x / args.splits : (int)blockIdx.x / CG;
     const int tile_step = args.splits > 1 ? args.num_tiles : (int)gridDim.x / CG;  // a slice has one tile
     const int kb_total = args.passes * args.num_kb;
@@ -230,28 +262,32 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         const bool elected = elect_one();
         bool ok = true;  // the elected thread's
         for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
-            int tm, tn;
-            tile_at(args, tile, &tm, &tn);
+            const Item it = item_at<SUBS>(args, tile);
+            const int tn = it.tn;
             const int which = EPI == EPI_STORE && tn >= args.n_tiles ? 1 : 0;
-            const int m0 = tm * (CG * ROWS) + (int)rank * ROWS;
+            const int m0 = it.tm * TILE_M + it.sub * (CG * ROWS) + (int)rank * ROWS;
             const int n0 = EPI == EPI_GATED ? tn * (block_n >> 1) : (tn - which * args.n_tiles) * block_n + (int)rank * own_n;
             for (int kb = kb_begin; kb < kb_end; ++kb) {
                 const int pass = kb / args.num_kb;  // 0 or 1
                 const int k0 = (kb - pass * args.num_kb) * BK;
                 const uint32_t full = CG == 2 ? map_to_cta(smem_u32(&bar_full[stage]), 0u) : smem_u32(&bar_full[stage]);
-                const uint32_t a_dst = stage_base + (uint32_t)stage * stage_bytes, b_dst = a_dst + P * a_plane;
+                const uint32_t a_dst = stage_base + (uint32_t)stage * stage_bytes, b_dst = a_dst + SUBS * P * a_plane;
                 // the weights of this half of the columns, of this pass, or one and the same
                 const CUtensorMap* map_b = (EPI == EPI_GATED ? (CG == 2 && rank == 1) : pass == 1) ? &map_b1 : &map_b0;
                 if (elected && ok && (ok = bounded_wait(smem_u32(&bar_empty[stage]), phase ^ 1u, abort_flag))) {
-                    if (leader) mbar_arrive_expect_tx(smem_u32(&bar_full[stage]), tx_bytes);
+                    if (leader) mbar_arrive_expect_tx(smem_u32(&bar_full[stage]), (uint32_t)it.subs * a_tx + b_tx);
 #pragma unroll
                     for (int p = 0; p < P; ++p) {
                         const int pa = pass * P + p, pb = which * P + p;
                         const uint32_t ad = a_dst + p * a_plane, bd = b_dst + p * b_plane;
-                        if (args.a_mn) {
-                            for (int i = 0; i < ROWS / 64; ++i) load3<CG>(ad + i * GROUP_BYTES, &map_a, full, m0 + 64 * i, k0, pa);
-                        } else {
-                            load3<CG>(ad, &map_a, full, k0, m0, pa);
+                        for (int u = 0; u < (SUBS == 1 ? 1 : it.subs); ++u) {
+                            const int mu = m0 + u * (CG * ROWS);
+                            const uint32_t au = ad + (uint32_t)u * (P * a_plane);
+                            if (args.a_mn) {
+                                for (int i = 0; i < ROWS / 64; ++i) load3<CG>(au + i * GROUP_BYTES, &map_a, full, mu + 64 * i, k0, pa);
+                            } else {
+                                load3<CG>(au, &map_a, full, k0, mu, pa);
+                            }
                         }
                         if (EPI == EPI_GATED && CG == 1) {
                             const int half = own_n >> 1;
@@ -302,7 +338,53 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             const bool elected = elect_one();
             bool ok = true;  // the elected thread's
             bool issued_any = false;
-            for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
+            if constexpr (SUBS == 2) {
+                // Both parts of a tile use each stage.  At its beginning and its end a part's MMAs of LEAD k-blocks go one after
+                // the other: the first part is complete, and read by the epilogue, while the second is still summed, and the
+                // next tile begins in the first part's columns while the second part's are read.
+                constexpr int LEAD = 2;
+                uint32_t part_phase[2] = {0u, 0u};
+                auto issue = [&](int at_stage, uint32_t at_phase, int part, bool first, bool wait) {
+                    const uint32_t base = stage_base + (uint32_t)at_stage * stage_bytes, a_addr = base + (uint32_t)part * a_plane;
+                    const uint32_t b_addr = base + 2 * a_plane;
+                    const uint64_t da = args.a_mn ? mn_desc(a_addr) : make_kmajor_sw128_desc(a_addr);
+                    const uint64_t db = args.b_mn ? mn_desc(b_addr) : make_kmajor_sw128_desc(b_addr);
+                    const uint32_t d = tmem_base + (uint32_t)part * acc_cols;
+                    if (elected && ok && (!wait || (ok = bounded_wait(smem_u32(&bar_full[at_stage]), at_phase, abort_flag)))) {
+                        if (wait) tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) mma<CG, KIND>(d, da + a_step * k, db + b_step * k, idesc, first && k == 0 ? 0u : 1u);
+                        issued_any = true;
+                    }
+                };
+                for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
+                    const int subs = item_at<SUBS>(args, tile).subs;
+                    for (int kb = kb_begin; kb < kb_end;) {
+                        // k-blocks of one part in a row
+                        const int run = kb == kb_begin || kb_end - kb <= LEAD ? min(LEAD, kb_end - kb) : 1;
+                        int st = stage;
+                        uint32_t ph = phase;
+                        for (int part = 0; part < subs; ++part) {
+                            if (kb == kb_begin) {
+                                if (elected && ok) ok = bounded_wait(smem_u32(&bar_acc_empty[part]), part_phase[part] ^ 1u, abort_flag);
+                                part_phase[part] ^= 1u;
+                                tc_fence_after();
+                            }
+                            st = stage;
+                            ph = phase;
+                            for (int j = 0; j < run; ++j) {
+                                issue(st, ph, part, kb + j == kb_begin, part == 0);
+                                if (part + 1 == subs && elected && ok) commit<CG>(smem_u32(&bar_empty[st]));
+                                if (++st == stages) { st = 0; ph ^= 1u; }
+                            }
+                            if (kb + run == kb_end && elected && ok) commit<CG>(smem_u32(&bar_acc_full[part]));
+                        }
+                        stage = st;
+                        phase = ph;
+                        kb += run;
+                    }
+                }
+            } else for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
                 int in_segment = 0;
                 for (int kb = kb_begin; kb < kb_end; ++kb) {
                     if (in_segment == 0 && elected && ok) ok = bounded_wait(smem_u32(&bar_acc_empty[acc]), acc_phase ^ 1u, abort_flag);
@@ -336,7 +418,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     ++in_segment;
                     if (kb + 1 == kb_end || (P == 3 && in_segment == args.seg_kb)) {
                         if (elected && ok) commit<CG>(smem_u32(&bar_acc_full[acc]));
-                        if (++acc == args.acc_stages) { acc = 0; acc_phase ^= 1u; }
+                        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
                         in_segment = 0;
                     }
                 }
@@ -353,34 +435,47 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- epilogue (warps 2..9)
-        // Two warps for each quadrant of tensor-memory lanes (32 rows) take alternate chunks of 32 columns; a gated tile's
-        // chunks are pairs, of g and of u.
+        // Two warps for each quadrant of tensor-memory lanes (32 rows) take alternate chunks of W columns; a gated tile's chunks
+        // are pairs, of g and of u.  The loop over chunks is rolled: a short call runs its code once, and fetching it unrolled
+        // took longer than the work.
+        constexpr int W = EPI == EPI_GATED || EPI == EPI_GRAD ? 16 : 32;
         const int quad = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const int n_chunks = block_n / 32 / (EPI == EPI_GATED ? 2 : 1);  // chunks, or pairs of them
+        const int n_chunks = block_n / W / (EPI == EPI_GATED ? 2 : 1);  // chunks, or pairs of them
         const int segments = P == 3 ? (kb_end - kb_begin + args.seg_kb - 1) / args.seg_kb : 1;
         const uint32_t pitch = (uint32_t)(block_n + 4) * 4u;  // of a partial tile's row: consecutive rows start 4 banks apart
         int acc = 0;
-        uint32_t acc_phase = 0;
+        uint32_t phases = 0;  // of the accumulators, a bit each
         bool ok = true;
+        auto wait_acc = [&]() {
+            const bool got = bounded_wait(smem_u32(&bar_acc_full[acc]), phases >> acc & 1u, abort_flag);
+            if (!__all_sync(0xffffffffu, got)) {
+                if (lane == 0) give_up(abort_flag, args.dev_status, DEV_STATUS_TIMEOUT_EPILOGUE);
+                return false;
+            }
+            phases ^= 1u << acc;
+            tc_fence_after();
+            return true;
+        };
+        auto release_acc = [&]() {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 2) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[acc]), 0u));
+                else mbar_arrive(smem_u32(&bar_acc_empty[acc]));
+            }
+        };
         for (int tile = first_tile; ok && tile < args.num_tiles; tile += tile_step) {
-            int tm, tn;
-            tile_at(args, tile, &tm, &tn);
+            const Item it = item_at<SUBS>(args, tile);
+            const int tn = it.tn;
             const int which = EPI == EPI_STORE && tn >= args.n_tiles ? 1 : 0;
-            const int64_t m0 = (int64_t)tm * (CG * ROWS) + (int)rank * ROWS;
+            const int64_t m0 = (int64_t)it.tm * TILE_M + it.sub * (CG * ROWS) + (int)rank * ROWS;
             const int n0 = EPI == EPI_GATED ? tn * (block_n >> 1) : (tn - which * args.n_tiles) * block_n;
-            float sum[P == 3 ? 2 : 1][32];  // P = 3: block_n is 128, a warp has two chunks
-            for (int segment = 0; segment < segments; ++segment) {
-                const bool got = bounded_wait(smem_u32(&bar_acc_full[acc]), acc_phase, abort_flag);
-                if (!__all_sync(0xffffffffu, got)) {
-                    if (lane == 0) give_up(abort_flag, args.dev_status, DEV_STATUS_TIMEOUT_EPILOGUE);
-                    ok = false;
-                    break;
-                }
-                tc_fence_after();
-                const uint32_t at = tmem_base + lanes + (uint32_t)acc * acc_cols;
-                const uint32_t acc_empty = CG == 2 ? map_to_cta(smem_u32(&bar_acc_empty[acc]), 0u) : smem_u32(&bar_acc_empty[acc]);
-                if constexpr (P == 3) {
+            float sum[P == 3 ? 2 : 1][32];  // P = 3: block_n is 128, a warp has two chunks of 32
+            if constexpr (P == 3) {
+                for (int segment = 0; segment < segments; ++segment) {
+                    if (!(ok = wait_acc())) break;
+                    const uint32_t at = tmem_base + lanes + (uint32_t)acc * acc_cols;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         uint32_t large[32];
@@ -392,32 +487,44 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                             for (int i = 0; i < 32; ++i) sum[j][i] = (segment | part ? sum[j][i] : 0.f) + __uint_as_float(large[i]);
                         }
                     }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (CG == 2) mbar_arrive_cluster(acc_empty);
-                        else mbar_arrive(acc_empty);
-                    }
-                } else if (args.splits == 1) {
+                    release_acc();
+                    acc ^= 1;
+                }
+            } else if (args.splits > 1) {
+                ok = wait_acc();
+            } else {
+                for (int u = 0; u < (SUBS == 1 ? 1 : it.subs); ++u) {
+                    if (SUBS == 2) acc = u;
+                    const int64_t row = m0 + u * (CG * ROWS) + quad * 32 + lane;
+                    float g[W], up[W];
+                    auto fetch = [&](int ch) {  // EPI_GRAD: g and u, on their way while the sums before are worked on
+                        const bool there = row < args.M && ch < n_chunks;
+                        const float* z = args.z + row * args.z_pitch + n0 + ch * W;
+                        load_f32(z, g, there ? args.N - n0 - ch * W : 0);
+                        load_f32(z + (int64_t)args.M * args.z_pitch, up, there ? args.N - n0 - ch * W : 0);
+                    };
+                    if constexpr (EPI == EPI_GRAD) fetch(half);
+                    if (!(ok = wait_acc())) break;
+                    const uint32_t at = tmem_base + lanes + (uint32_t)acc * acc_cols;
+#pragma unroll 1
                     for (int ch = half; ch < n_chunks; ch += 2) {
-                        uint32_t first[32], up[EPI == EPI_GATED ? 32 : 1];
-                        tc_ld_32x32(at + (uint32_t)ch * 32u, first);
-                        if constexpr (EPI == EPI_GATED) tc_ld_32x32(at + (uint32_t)(block_n / 2 + ch * 32), up);
+                        uint32_t first[W], second[EPI == EPI_GATED ? W : 1];
+                        ld_columns(at + (uint32_t)(ch * W), first);
+                        if constexpr (EPI == EPI_GATED) ld_columns(at + (uint32_t)(block_n / 2 + ch * W), second);
                         tc_ld_wait();
-                        if (ch + 2 >= n_chunks) {
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) {
-                                if (CG == 2) mbar_arrive_cluster(acc_empty);
-                                else mbar_arrive(acc_empty);
-                            }
-                        }
-                        if constexpr (EPI == EPI_GATED) finish<P, EPI, 32>(args, which, m0 + quad * 32 + lane, n0 + ch * 32, first, up);
-                        else finish<P, EPI, 32>(args, which, m0 + quad * 32 + lane, n0 + ch * 32, first, first);
+                        if (ch + 2 >= n_chunks) release_acc();
+                        if constexpr (EPI == EPI_GATED) finish<P, EPI, W>(args, which, row, n0 + ch * W, first, second);
+                        else if constexpr (EPI == EPI_GRAD) {
+                            float z0[W], z1[W];
+#pragma unroll
+                            for (int i = 0; i < W; ++i) { z0[i] = g[i]; z1[i] = up[i]; }
+                            fetch(ch + 2);
+                            finish_gradient<P, W>(args, row, n0 + ch * W, first, z0, z1);
+                        } else finish<P, EPI, W>(args, which, row, n0 + ch * W, first, first);
                         __syncwarp();
                     }
+                    if (SUBS == 1) acc ^= 1;
                 }
-                if (++acc == args.acc_stages) { acc = 0; acc_phase ^= 1u; }
             }
             if constexpr (P == 3) {
                 if (ok && args.splits == 1) {
@@ -535,9 +642,9 @@ tfjsb_status encode(tfjsb_ctx* ctx, CUtensorMap* map, const Operand& o, Kind kin
     return TFJSB_OK;
 }
 
-template <int CG, int P, int KIND, int EPI>
+template <int CG, int P, int KIND, int EPI, int SUBS = 1>
 cudaError_t launch(const CUtensorMap* maps, const Args& args, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
-    auto* kernel = &dense_kernel<CG, P, KIND, EPI>;
+    auto* kernel = &dense_kernel<CG, P, KIND, EPI, SUBS>;
     cudaError_t e = smem_attr_once(reinterpret_cast<const void*>(kernel), tile::SMEM_LIMIT - 2048);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -567,6 +674,13 @@ cudaError_t launch(const CUtensorMap* maps, const Args& args, int grid, size_t s
     return e;
 }
 
+cudaError_t launch_wide(const Product& p, const CUtensorMap* maps, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
+    if (p.kind == KIND_INT8) return launch<2, 1, KIND_INT8, EPI_SCALE, 2>(maps, p.args, grid, smem, s, launches);
+    if (p.epilogue == EPI_GATED) return launch<2, 1, KIND_BF16, EPI_GATED, 2>(maps, p.args, grid, smem, s, launches);
+    if (p.epilogue == EPI_GRAD) return launch<2, 1, KIND_BF16, EPI_GRAD, 2>(maps, p.args, grid, smem, s, launches);
+    return launch<2, 1, KIND_BF16, EPI_STORE, 2>(maps, p.args, grid, smem, s, launches);
+}
+
 template <int CG>
 cudaError_t launch_any(const Product& p, const CUtensorMap* maps, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
     if (p.kind == KIND_INT8) return launch<CG, 1, KIND_INT8, EPI_SCALE>(maps, p.args, grid, smem, s, launches);
@@ -580,19 +694,24 @@ cudaError_t launch_any(const Product& p, const CUtensorMap* maps, int grid, size
     return launch<CG, 3, KIND_BF16, EPI_STORE>(maps, p.args, grid, smem, s, launches);
 }
 
-// Which kernel: CTA pairs or single CTAs, columns of a tile, slices of K.
-struct Shape { int cg, block_n, splits; };
+// Which kernel: CTA pairs or single CTAs, columns of a tile, slices of K, parts of a tile's rows.
+struct Shape { int cg, block_n, splits, subs; };
 
-int64_t tiles_of(const Product& p, int cg, int block_n) {
-    const int64_t columns = p.epilogue == EPI_GATED ? block_n / 2 : block_n;
-    return ((p.args.M + cg * ROWS - 1) / (cg * ROWS)) * ((p.args.N + columns - 1) / columns) * p.args.outputs;
+int64_t tiles_of(const Product& p, int cg, int block_n, int subs = 1) {
+    const int64_t columns = p.epilogue == EPI_GATED ? block_n / 2 : block_n, rows = cg * ROWS * subs;
+    return ((p.args.M + rows - 1) / rows) * ((p.args.N + columns - 1) / columns) * p.args.outputs;
 }
 
 // Estimated cycles: rounds of tiles x k-blocks x cycles of a k-block, and what a tile and a launch cost beside them.  A k-block's
 // MMAs take 2 cycles a column; single CTAs are bound by their shared memory (operand rows written and read) instead.
 double cost(const Product& p, const Shape& c, int sm_count) {
     const int kb = (p.args.K + (p.kind == KIND_BF16 ? 63 : 127)) / (p.kind == KIND_BF16 ? 64 : 128) * p.args.passes;
-    const double per_kb = (c.cg == 2 ? 2.1 * c.block_n + 20 : 2.0 * c.block_n + 256) * (p.planes == 3 ? 6 : 1);
+    if (c.subs == 2) {
+        const int64_t tiles = tiles_of(p, 2, 256, 2), slots = sm_count / 2, rest = tiles % slots;
+        const double rounds = tiles / slots + (rest == 0 ? 0. : 2 * rest <= slots ? 0.6 : 1.);
+        return rounds * kb * 1150 + 4000;
+    }
+    const double per_kb = (c.cg == 2 ? 2.6 * c.block_n + 20 : 2.0 * c.block_n + 256) * (p.planes == 3 ? 6 : 1);
     const int64_t tiles = tiles_of(p, c.cg, c.block_n);
     const int64_t rounds = c.splits > 1 ? 1 : (tiles + sm_count / c.cg - 1) / (sm_count / c.cg);
     const int own_kb = (kb + c.splits - 1) / c.splits;
@@ -600,8 +719,10 @@ double cost(const Product& p, const Shape& c, int sm_count) {
 }
 
 Shape choose(const Product& p, int sm_count) {
-    const char* forced = getenv("TFJSB_DENSE_SHAPE");  // "cta group,columns,slices", wherever the product allows it
-    Shape best = {1, 128, 1};
+    const char* forced = getenv("TFJSB_DENSE_SHAPE");  // for tests: "CTA group,columns,slices,parts", wherever the product allows it
+    int f[4];
+    const bool force = forced && sscanf(forced, "%d,%d,%d,%d", &f[0], &f[1], &f[2], &f[3]) == 4;
+    Shape best = {1, 128, 1, 1};
     double least = -1;
     const int kb = (p.args.K + (p.kind == KIND_BF16 ? 63 : 127)) / (p.kind == KIND_BF16 ? 64 : 128) * p.args.passes;
     for (int cg = 1; cg <= 2; ++cg)
@@ -613,13 +734,12 @@ Shape choose(const Product& p, int sm_count) {
                 // at least four k-blocks a slice, none without any, one wave
                 const int each = (kb + splits - 1) / splits;
                 if (splits > 1 && (each < 4 || each * (splits - 1) >= kb || tiles * splits > sm_count)) continue;
-                const Shape c = {cg, bn, splits};
-                if (forced) {
-                    int f[3];
-                    if (sscanf(forced, "%d,%d,%d", &f[0], &f[1], &f[2]) == 3 && f[0] == cg && f[1] == bn && f[2] == splits) return c;
+                for (int subs = 1; subs <= (cg == 2 && bn == 256 && p.planes == 1 ? 2 : 1); ++subs) {
+                    const Shape c = {cg, bn, splits, subs};
+                    if (force && f[0] == cg && f[1] == bn && f[2] == splits && f[3] == subs) return c;
+                    const double cycles = cost(p, c, sm_count);
+                    if (least < 0 || cycles < least) { least = cycles; best = c; }
                 }
-                const double cycles = cost(p, c, sm_count);
-                if (least < 0 || cycles < least) { least = cycles; best = c; }
             }
         }
     return best;
@@ -634,23 +754,29 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     const int bk = p.kind == KIND_BF16 ? 64 : 128;
     a.block_n = c.block_n;
     a.splits = c.splits;
-    a.acc_stages = 2;
     a.seg_kb = 2;  // 8 additions to an accumulator of large products
     a.num_kb = (a.K + bk - 1) / bk;
     a.kb_per_split = (a.num_kb * a.passes + c.splits - 1) / c.splits;
-    a.m_tiles = (a.M + c.cg * ROWS - 1) / (c.cg * ROWS);
+    a.m_tiles = (a.M + c.cg * ROWS * c.subs - 1) / (c.cg * ROWS * c.subs);
     const int columns = p.epilogue == EPI_GATED ? c.block_n / 2 : c.block_n;
     a.n_tiles = (a.N + columns - 1) / columns;
-    const int64_t tiles = tiles_of(p, c.cg, c.block_n);
-    if (tiles >= (1LL << 31)) return fail(ctx, TFJSB_ERR_UNSUPPORTED, "too many tiles");
+    const int64_t slots = ctx->sm_count / c.cg;
+    int64_t tiles = tiles_of(p, c.cg, c.block_n, c.subs);
+    if (tiles >= (1LL << 30)) return fail(ctx, TFJSB_ERR_UNSUPPORTED, "too many tiles");
+    a.whole_tiles = (int)tiles;
+    if (c.subs == 2 && 2 * (tiles % slots) <= slots) {  // a last round of few tiles: their parts as tiles of their own
+        a.whole_tiles -= (int)(tiles % slots);
+        tiles += tiles % slots;
+    }
     a.num_tiles = (int)tiles;
+    a.band = 8 / c.subs;
     a.a_mn = p.a.mn;
     a.b_mn = p.b[0].mn;
     // of a matrix of less rows than a tile only those are copied (a multiple of 8, the swizzle's period): the others' sums are not stored
     a.a_rows = !p.a.mn && a.M < ROWS ? (a.M + 7) / 8 * 8 : ROWS;
     a.dev_status = ctx->dev_status;
     const int own_n = c.block_n / c.cg;
-    const int stage_bytes = p.planes * (A_BYTES + own_n * 128);
+    const int stage_bytes = p.planes * (c.subs * A_BYTES + own_n * 128);
     int stages = (tile::SMEM_LIMIT - 2048 - 1024) / stage_bytes;
     a.stages = stages < MAX_STAGES ? stages : MAX_STAGES;
     const size_t smem = 1024 + (size_t)a.stages * stage_bytes;
@@ -664,9 +790,9 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     } else {
         maps[2] = maps[1];
     }
-    const int64_t slots = ctx->sm_count / c.cg;
     const int grid = (int)(c.splits > 1 ? tiles * c.splits : (tiles < slots ? tiles : slots) * c.cg);
-    const cudaError_t e = c.cg == 2 ? launch_any<2>(p, maps, grid, smem, s, &ctx->launches) : launch_any<1>(p, maps, grid, smem, s, &ctx->launches);
+    const cudaError_t e = c.subs == 2 ? launch_wide(p, maps, grid, smem, s, &ctx->launches)
+                          : c.cg == 2 ? launch_any<2>(p, maps, grid, smem, s, &ctx->launches) : launch_any<1>(p, maps, grid, smem, s, &ctx->launches);
     return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "dense product launch");
 }
 

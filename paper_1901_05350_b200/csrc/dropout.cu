@@ -5,9 +5,8 @@
 // are whole numbers, so keeping one is a comparison, word >= ceil(rate 2^32), and needs no conversion.
 //
 // A thread has eight consecutive elements, 16 or 32 bytes of each tensor.  Without broadcasting their words are two whole blocks.  With
-// it (a mask of fewer dimensions) an element's index in the mask is worked out for the first of the eight; as long as the eight lie in
-// one row of the innermost dimension their words are one (that dimension is broadcast) or eight in a row, out of three blocks (it is not).  Groups that
-// cross the end of a row take element by element.
+// it (a mask of fewer dimensions) an element's index in the mask is worked out for the first of the eight; those that lie in one row of the
+// innermost dimension share one word (that dimension is broadcast) or have words in a row, out of two or three blocks (it is not).
 #include <cmath>
 
 #include <cuda_bf16.h>
@@ -65,48 +64,65 @@ __device__ __forceinline__ uint64_t mask_index(const DropoutArgs& a, uint64_t i,
     return m;
 }
 
-// Which of the `left` (at most eight) elements from i on are kept, a bit each.
+// Eight words of the stream from word m on (m may be "negative": words before the first mean nothing), out of two blocks or,
+// where m is no multiple of four, three.
+__device__ __forceinline__ void run_of_words(const DropoutArgs& a, uint64_t m, uint32_t (&w)[8]) {
+    uint32_t v[12];
+    const uint64_t block = (uint64_t)((int64_t)m >> 2);
+    const uint32_t r = (uint32_t)m & 3u;
+#pragma unroll
+    for (int b = 0; b < 3; ++b) {
+        if (b == 2 && r == 0) break;
+        uint32_t q[4];
+        philox(a, block + b, q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * b + e] = q[e];
+    }
+    if (r & 1u) {
+#pragma unroll
+        for (int e = 0; e < 11; ++e) v[e] = v[e + 1];
+    }
+    if (r & 2u) {
+#pragma unroll
+        for (int e = 0; e < 9; ++e) v[e] = v[e + 2];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = v[e];
+}
+
+// The words of the `left` (at most eight) elements from i on.
 template <bool BROADCAST, typename I>
-__device__ __forceinline__ uint32_t kept(const DropoutArgs& a, uint64_t i, int left) {
-    uint32_t bits = 0;
+__device__ __forceinline__ void words_of(const DropoutArgs& a, uint64_t i, int left, uint32_t (&w)[8]) {
     if (!BROADCAST) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            uint32_t w[4];
-            philox(a, (i >> 2) + b, w);
+            uint32_t q[4];
+            philox(a, (i >> 2) + b, q);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) bits |= (w[e] >= a.threshold ? 1u : 0u) << (4 * b + e);
+            for (int e = 0; e < 4; ++e) w[4 * b + e] = q[e];
         }
-        return bits;
+        return;
     }
-    uint64_t inner = 0;
-    const uint64_t m = mask_index<I>(a, i, &inner);
-    if (inner + (uint64_t)left <= a.extent[0]) {
+    // run by run: the elements that lie in one row of the innermost dimension
+    for (int e0 = 0; e0 < left;) {
+        uint64_t inner = 0;
+        const uint64_t m = mask_index<I>(a, i + e0, &inner);
+        const int end = (uint64_t)(left - e0) < a.extent[0] - inner ? left : e0 + (int)(a.extent[0] - inner);
+        uint32_t u[8];
         if (a.step[0] == 0) {
-            uint32_t w[4];
-            philox(a, m >> 2, w);
-            const int at = (int)(m & 3);
-            const uint32_t v = at == 0 ? w[0] : at == 1 ? w[1] : at == 2 ? w[2] : w[3];
-            return v >= a.threshold ? 0xffu : 0u;
+            uint32_t q[4];
+            philox(a, m >> 2, q);
+            const uint32_t v = (m & 2) ? ((m & 1) ? q[3] : q[2]) : ((m & 1) ? q[1] : q[0]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = v;
+        } else {
+            run_of_words(a, m - (uint64_t)e0, u);
         }
 #pragma unroll
-        for (int b = 0; b < 3; ++b) {
-            uint32_t w[4];
-            philox(a, (m >> 2) + b, w);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) bits |= (w[e] >= a.threshold ? 1u : 0u) << (4 * b + e);
-        }
-        return bits >> (m & 3);
+        for (int e = 0; e < 8; ++e)
+            if (e >= e0 && e < end) w[e] = u[e];
+        e0 = end;
     }
-    for (int e = 0; e < left; ++e) {
-        uint32_t w[4];
-        const uint64_t k = mask_index<I>(a, i + e, &inner);
-        philox(a, k >> 2, w);
-        const int at = (int)(k & 3);
-        const uint32_t v = at == 0 ? w[0] : at == 1 ? w[1] : at == 2 ? w[2] : w[3];
-        bits |= (v >= a.threshold ? 1u : 0u) << e;
-    }
-    return bits;
 }
 
 template <bool F32>
@@ -139,11 +155,12 @@ __global__ void __launch_bounds__(BLOCK) dropout_kernel(const __grid_constant__ 
         float x[8], r[8];
         load8<F32>(a.x, i, left, x);
         if (RESIDUAL) load8<F32>(a.residual, i, left, r);
-        const uint32_t keep = kept<BROADCAST, I>(a, (uint64_t)i, left);
+        uint32_t w[8];
+        words_of<BROADCAST, I>(a, (uint64_t)i, left, w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if (RESIDUAL) x[e] = (keep >> e & 1u) ? fmaf(x[e], a.scale, r[e]) : r[e];
-            else x[e] = (keep >> e & 1u) ? x[e] * a.scale : 0.f;
+            if (RESIDUAL) x[e] = w[e] >= a.threshold ? fmaf(x[e], a.scale, r[e]) : r[e];
+            else x[e] = w[e] >= a.threshold ? x[e] * a.scale : 0.f;
         }
         if (F32) dense::store_f32(static_cast<float*>(a.out) + i, x, left);
         else dense::store_bf16(static_cast<__nv_bfloat16*>(a.out) + i, x, left);

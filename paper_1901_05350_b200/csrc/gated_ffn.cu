@@ -69,6 +69,7 @@ struct Sizes {
     bool repack_x, repack_up, repack_down, repack_dy;  // operands that are copied: x; w_gate and w_up; w_down; dy
     int64_t x_bytes, w_bytes, wd_bytes, dy_bytes;      // of such a copy
     int64_t h_bytes, z_bytes, grad_bytes;              // grad: dg and du
+    int64_t few;                                       // h of the form for few tokens, fp32
     int64_t forward, backward;
 };
 
@@ -98,7 +99,8 @@ tfjsb_status sizes_of(const tfjsb_ffn* f, Sizes* s, std::string* why) {
     s->z_bytes = up256(s->T * s->fp * 8);
     s->grad_bytes = up256(s->T * s->fp * 2 * e);
     const int64_t weights = (s->repack_x ? s->x_bytes : 0) + (s->repack_up ? 2 * s->w_bytes : 0) + (s->repack_down ? s->wd_bytes : 0);
-    s->forward = weights + s->h_bytes;
+    s->few = s->T <= FEW_ROWS ? up256(s->T * s->F * 4) : 0;
+    s->forward = weights + s->h_bytes > s->few ? weights + s->h_bytes : s->few;
     s->backward = weights + (s->repack_dy ? s->dy_bytes : 0) + s->grad_bytes;
     return TFJSB_OK;
 }
@@ -211,6 +213,11 @@ tfjsb_status tfjsb_gated_ffn(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, const void* x
                        {w_down, s.F * s.Do * size, "w_down"}};
     if ((st = check_ranges(ctx, r, 8, 4, 6u)) != TFJSB_OK) return st;
     const cudaStream_t stm = static_cast<cudaStream_t>(stream);
+    if (!h && s.T <= FEW_ROWS) {
+        float* few = static_cast<float*>(workspace);
+        if ((st = few_rows_gated(ctx, s.planes == 3, x, w_gate, w_up, ffn->gate, few, s.T, s.F, s.D, stm)) != TFJSB_OK) return st;
+        return few_rows_down(ctx, s.planes == 3, few, w_down, y, s.T, s.Do, s.F, stm);
+    }
 
     Arena arena{static_cast<uint8_t*>(workspace)};
     LayoutArgs layout;

@@ -158,3 +158,55 @@ def test_dense_int8(ctx, shape, dtype):
     # the same as the two calls, bit for bit
     a, s = ctx.quantize_int8(x)
     assert torch.equal(y, ctx.matmul_int8(a, s, w, w_scale, bias=bias, act="relu", out_dtype=dtype))
+
+
+# ---- every kernel shape -------------------------------------------------------------------------------------------
+
+KERNELS = ["1,64,1,1", "1,128,1,1", "1,256,1,1", "2,128,1,1", "2,256,1,1", "2,256,1,2", "1,64,2,1", "1,128,2,1", "1,128,4,1", "1,64,8,1", "1,128,8,1"]
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_ffn_on_every_kernel(ctx, monkeypatch, kernel, dtype):
+    """CTA group, columns of a tile, slices of K and parts of a tile's rows as the variable says, wherever a product allows it."""
+    monkeypatch.setenv("TFJSB_DENSE_SHAPE", kernel)
+    for shape in ((200, 600, 328, 136), (37, 1100, 513, 260)):
+        gate = "silu"
+        x, wg, wu, wd, dy = block(40, *shape, dtype)
+        want = [ref.gated_ffn(x, wg, wu, wd, gate), *ref.gated_ffn_gradients(x, wg, wu, wd, dy, gate)]
+        bounds = ref.gated_ffn_bounds(x, wg, wu, wd, dy, gate)
+        y, h, z = ctx.gated_ffn(x, wg, wu, wd, gate=gate, save=True)
+        grads = ctx.gated_ffn_backprop(x, wg, wu, wd, h, z, dy, gate=gate)
+        ctx.check_device_status()
+        for got, w, b, what in zip((y, *grads), want, bounds, ("y", "dx", "dw_gate", "dw_up", "dw_down")):
+            check_ffn(got, w, b, dtype, (what, shape))
+
+
+@pytest.mark.parametrize("kernel", ["2,256,1,1", "2,256,1,2"])
+@pytest.mark.parametrize("shape", [(2600, 72, 5000, 40), (5130, 1300, 136, 1024)], ids=str)
+def test_ffn_with_several_rounds_of_tiles(ctx, monkeypatch, kernel, shape):
+    """More tiles than CTA pairs: accumulators in turn, a last round of few tiles whose parts go to pairs of their own, rows that end in the
+    first part of a tile."""
+    monkeypatch.setenv("TFJSB_DENSE_SHAPE", kernel)
+    x, wg, wu, wd, dy = block(50, *shape, torch.bfloat16)
+    want = [ref.gated_ffn(x, wg, wu, wd, "gelu"), *ref.gated_ffn_gradients(x, wg, wu, wd, dy, "gelu")]
+    bounds = ref.gated_ffn_bounds(x, wg, wu, wd, dy, "gelu")
+    y, h, z = ctx.gated_ffn(x, wg, wu, wd, gate="gelu", save=True)
+    grads = ctx.gated_ffn_backprop(x, wg, wu, wd, h, z, dy, gate="gelu")
+    ctx.check_device_status()
+    for got, w, b, what in zip((y, *grads), want, bounds, ("y", "dx", "dw_gate", "dw_up", "dw_down")):
+        check_ffn(got, w, b, torch.bfloat16, what)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_int8_on_every_kernel(ctx, monkeypatch, kernel):
+    """Whole numbers: the sums have to be exact on each."""
+    monkeypatch.setenv("TFJSB_DENSE_SHAPE", kernel)
+    for M, K, N in ((300, 4208, 328), (37, 2064, 513), (1400, 272, 8200)):
+        gen = torch.Generator(device="cuda").manual_seed(M)
+        a = torch.randint(-128, 128, (M, K), generator=gen, device="cuda").to(torch.int8)
+        w = torch.randint(-128, 128, (N, K), generator=gen, device="cuda").to(torch.int8)
+        one_m, one_n = torch.ones(M, device="cuda"), torch.ones(N, device="cuda")
+        y = ctx.matmul_int8(a, one_m, w, one_n, out_dtype=torch.float32)
+        ctx.check_device_status()
+        assert torch.equal(y, (a.double() @ w.double().T).float())
