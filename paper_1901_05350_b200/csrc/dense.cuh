@@ -36,6 +36,7 @@ struct Args {
     int a_mn = 0, b_mn = 0, a_rows = 0;
     void* out[2] = {nullptr, nullptr};
     int64_t out_pitch = 0, out_plane = 0;  // elements
+    int out_mapped = 0;                    // results leave through shared memory
     float* z = nullptr;                    // [2][M][z_pitch]
     int64_t z_pitch = 0;
     int gate = 0;

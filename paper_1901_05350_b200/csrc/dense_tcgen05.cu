@@ -96,6 +96,38 @@ __device__ __forceinline__ uint4 lds4_cluster(uint32_t addr) {
 __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[32]) { tc_ld_32x32(at, r); }
 __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[16]) { tc_ld_cols(at, r); }
 
+struct Maps {
+    CUtensorMap a, b[2];
+    CUtensorMap out[2];  // results that are stored from shared memory
+    CUtensorMap z;
+};
+
+// Shared memory of an epilogue warp: chunks of 32 rows on their way out, or of g and u on their way in (two buffers).
+template <int P, int EPI> constexpr int SLAB_BYTES = P == 3 ? 0 : EPI == EPI_GRAD ? 8192 : 4096;
+
+// 16-byte piece j of row r of a chunk whose rows are 64 bytes in the 64-byte swizzle, or 128 bytes in the 128-byte one.
+__device__ __forceinline__ uint32_t piece64(int r, int j) { return (uint32_t)(r * 64 + ((j ^ (r >> 1 & 3)) << 4)); }
+__device__ __forceinline__ uint32_t piece128(int r, int j) { return (uint32_t)(r * 128 + ((j ^ (r & 7)) << 4)); }
+__device__ __forceinline__ void sts16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// A row of 16 or 32 fp32 values, or of 32 that are rounded to bfloat16, into the slab.
+__device__ __forceinline__ void stage_row(uint32_t slab, int r, const uint32_t (&v)[16]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sts16(slab + piece64(r, j), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+}
+__device__ __forceinline__ void stage_row_f32(uint32_t slab, int r, const float (&v)[32]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        sts16(slab + piece128(r, j), __float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
+}
+__device__ __forceinline__ void stage_row_bf16(uint32_t slab, int r, const float (&v)[32]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        sts16(slab + piece64(r, j), pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]), pack_bf16(v[8 * j + 4], v[8 * j + 5]),
+              pack_bf16(v[8 * j + 6], v[8 * j + 7]));
+}
+
 // Tile number -> (tile row, tile column), in bands of `band` tile rows, down a band's columns one after the other.
 __device__ __forceinline__ void tile_at(const Args& a, int tile, int* m, int* n) {
     const int columns = a.n_tiles * a.outputs;
@@ -141,6 +173,21 @@ __device__ __forceinline__ void finish_gradient(const Args& a, int64_t row, int 
     store_planes<P>(dst + P * a.out_plane, a.out_plane, du, left);
 }
 
+// act(sum a_scale b_scale + bias); bias is 0 where there is none
+template <int W>
+__device__ __forceinline__ void scaled(const Args& a, float row_scale, const uint32_t (&sum)[W], const float (&scale)[W], const float (&bias)[W],
+                                       float (&v)[W]) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = fmaf((float)(int)sum[i] * row_scale, scale[i], bias[i]);
+    if (a.act == TFJSB_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = relu_nan(v[i]);
+    } else if (a.act == TFJSB_ACT_RELU6) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = relu6_nan(v[i]);
+    }
+}
+
 template <int P, int EPI, int W>
 __device__ __forceinline__ void finish(const Args& a, int which, int64_t row, int col, const uint32_t (&first)[W], const uint32_t (&second)[W]) {
     const int left = a.N - col;  // columns that exist
@@ -152,24 +199,17 @@ __device__ __forceinline__ void finish(const Args& a, int which, int64_t row, in
         if constexpr (P == 1) store_bf16(static_cast<__nv_bfloat16*>(a.out[which]) + row * a.out_pitch + col, v, left);
         else store_f32(static_cast<float*>(a.out[which]) + row * a.out_pitch + col, v, left);
     } else if constexpr (EPI == EPI_SCALE) {
-        const float s = load_global(a.a_scale + row);
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if (i < left) {
-                float r = (float)(int)first[i] * s * load_global(a.b_scale + col + i);
-                if (a.bias) r += load_global(a.bias + col + i);
-                v[i] = apply_act(r, a.act);
-            } else {
-                v[i] = 0.f;
-            }
-        }
+        float scale[W], bias[W];
+        load_f32(a.b_scale + col, scale, left);
+        load_f32(a.bias + col, bias, a.bias ? left : 0);
+        scaled(a, load_global(a.a_scale + row), first, scale, bias, v);
         if (a.out_bf16) store_bf16(static_cast<__nv_bfloat16*>(a.out[0]) + row * a.out_pitch + col, v, left);
         else store_f32(static_cast<float*>(a.out[0]) + row * a.out_pitch + col, v, left);
     } else if constexpr (EPI == EPI_GATED) {
         float g[W], u[W];
 #pragma unroll
         for (int i = 0; i < W; ++i) { g[i] = __uint_as_float(first[i]); u[i] = __uint_as_float(second[i]); }
-        if (a.z) {
+        if (a.z && (P == 3 || W == 8)) {  // otherwise copied from shared memory
             float* z = a.z + row * a.z_pitch + col;
             store_f32(z, g, left);
             store_f32(z + (int64_t)a.M * a.z_pitch, u, left);
@@ -187,14 +227,16 @@ __device__ __forceinline__ void finish(const Args& a, int which, int64_t row, in
 
 template <int CG, int P, int KIND, int EPI, int SUBS>
 __global__ void __launch_bounds__(THREADS, 1)
-dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1,
-             const __grid_constant__ Args args) {
+dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args args) {
+    const CUtensorMap &map_a = maps.a, &map_b0 = maps.b[0], &map_b1 = maps.b[1];
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_full[MAX_STAGES];  // CG = 2: used in the even CTA only
     __shared__ __align__(8) uint64_t bar_empty[MAX_STAGES];
     __shared__ __align__(8) uint64_t bar_acc_full[2];
     __shared__ __align__(8) uint64_t bar_acc_empty[2];      // CG = 2: used in the even CTA only
     __shared__ __align__(8) uint64_t bar_drain;
+    constexpr int SLAB = SLAB_BYTES<P, EPI>;
+    __shared__ __align__(8) uint64_t bar_z[EPI == EPI_GRAD && P == 1 ? 16 : 1];  // of an epilogue warp's two buffers
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag_s;
 
@@ -228,6 +270,8 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             mbar_init(smem_u32(&bar_acc_empty[s]), 8 * CG);  // the epilogue warps
         }
         mbar_init(smem_u32(&bar_drain), 1);
+        if (EPI == EPI_GRAD && P == 1)
+            for (int i = 0; i < 16; ++i) mbar_init(smem_u32(&bar_z[i]), 1);
         abort_flag_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
@@ -444,6 +488,10 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         const int n_chunks = block_n / W / (EPI == EPI_GATED ? 2 : 1);  // chunks, or pairs of them
         const int segments = P == 3 ? (kb_end - kb_begin + args.seg_kb - 1) / args.seg_kb : 1;
         const uint32_t pitch = (uint32_t)(block_n + 4) * 4u;  // of a partial tile's row: consecutive rows start 4 banks apart
+        const int ew = warp - 2;
+        const uint32_t slab = stage_base + (uint32_t)stages * stage_bytes + (uint32_t)(ew * SLAB);
+        int z_fetch = 0, z_use = 0, z_out = 0;  // buffers of the slab, copies in flight
+        uint32_t z_phases = 0;
         int acc = 0;
         uint32_t phases = 0;  // of the accumulators, a bit each
         bool ok = true;
@@ -495,34 +543,114 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             } else {
                 for (int u = 0; u < (SUBS == 1 ? 1 : it.subs); ++u) {
                     if (SUBS == 2) acc = u;
-                    const int64_t row = m0 + u * (CG * ROWS) + quad * 32 + lane;
-                    float g[W], up[W];
-                    auto fetch = [&](int ch) {  // EPI_GRAD: g and u, on their way while the sums before are worked on
-                        const bool there = row < args.M && ch < n_chunks;
-                        const float* z = args.z + row * args.z_pitch + n0 + ch * W;
-                        load_f32(z, g, there ? args.N - n0 - ch * W : 0);
-                        load_f32(z + (int64_t)args.M * args.z_pitch, up, there ? args.N - n0 - ch * W : 0);
+                    const int64_t row0 = m0 + u * (CG * ROWS) + quad * 32, row = row0 + lane;
+                    const bool rows_live = row0 < args.M;
+                    float c0[W], c1[W];  // EPI_SCALE: scales and biases of the next chunk's columns, on their way while a chunk is worked on
+                    const float row_scale = EPI == EPI_SCALE && row < args.M ? load_global(args.a_scale + row) : 0.f;
+                    auto fetch = [&](int ch) {
+                        const int col = n0 + ch * W;
+                        if constexpr (EPI == EPI_SCALE) {
+                            const int left = ch < n_chunks ? args.N - col : 0;
+                            load_f32(args.b_scale + col, c0, left);
+                            load_f32(args.bias + col, c1, args.bias ? left : 0);
+                        } else if constexpr (EPI == EPI_GRAD) {  // g and u of 32 rows
+                            if (ch >= n_chunks || !rows_live || col >= args.N) return;
+                            if (lane == 0) {
+                                const uint32_t bar = smem_u32(&bar_z[ew * 2 + z_fetch]), to = slab + (uint32_t)z_fetch * 4096u;
+                                mbar_arrive_expect_tx(bar, 4096u);
+                                tma_load_3d(to, &maps.z, bar, col, (int)row0, 0);
+                                tma_load_3d(to + 2048u, &maps.z, bar, col, (int)row0, 1);
+                            }
+                            z_fetch ^= 1;
+                            ++z_out;
+                        }
                     };
-                    if constexpr (EPI == EPI_GRAD) fetch(half);
+                    fetch(half);
                     if (!(ok = wait_acc())) break;
                     const uint32_t at = tmem_base + lanes + (uint32_t)acc * acc_cols;
 #pragma unroll 1
                     for (int ch = half; ch < n_chunks; ch += 2) {
+                        const int col = n0 + ch * W;
                         uint32_t first[W], second[EPI == EPI_GATED ? W : 1];
                         ld_columns(at + (uint32_t)(ch * W), first);
                         if constexpr (EPI == EPI_GATED) ld_columns(at + (uint32_t)(block_n / 2 + ch * W), second);
                         tc_ld_wait();
                         if (ch + 2 >= n_chunks) release_acc();
-                        if constexpr (EPI == EPI_GATED) finish<P, EPI, W>(args, which, row, n0 + ch * W, first, second);
-                        else if constexpr (EPI == EPI_GRAD) {
-                            float z0[W], z1[W];
-#pragma unroll
-                            for (int i = 0; i < W; ++i) { z0[i] = g[i]; z1[i] = up[i]; }
+                        if (!rows_live || col >= args.N) continue;
+                        if constexpr (EPI == EPI_GATED) {
+                            if (args.z) {
+                                if (lane == 0) tma_store_wait_read<0>();
+                                __syncwarp();
+                                stage_row(slab, lane, first);
+                                stage_row(slab + 2048u, lane, second);
+                                fence_async_smem();
+                                __syncwarp();
+                                if (lane == 0) {
+                                    tma_store_3d(&maps.z, slab, col, (int)row0, 0);
+                                    tma_store_3d(&maps.z, slab + 2048u, col, (int)row0, 1);
+                                    tma_store_commit();
+                                }
+                            }
+                            finish<P, EPI, W>(args, which, row, col, first, second);
+                        } else if constexpr (EPI == EPI_GRAD) {
                             fetch(ch + 2);
-                            finish_gradient<P, W>(args, row, n0 + ch * W, first, z0, z1);
-                        } else finish<P, EPI, W>(args, which, row, n0 + ch * W, first, first);
+                            const bool got = bounded_wait(smem_u32(&bar_z[ew * 2 + z_use]), z_phases >> z_use & 1u, abort_flag);
+                            if (!__all_sync(0xffffffffu, got)) {
+                                if (lane == 0) give_up(abort_flag, args.dev_status, DEV_STATUS_TIMEOUT_EPILOGUE);
+                                ok = false;
+                                break;
+                            }
+                            z_phases ^= 1u << z_use;
+                            --z_out;
+                            const uint32_t from = slab + (uint32_t)z_use * 4096u;
+                            z_use ^= 1;
+#pragma unroll
+                            for (int j = 0; j < W / 4; ++j) {
+                                const float4 g = tile::lds4(from + piece64(lane, j)), w = tile::lds4(from + 2048u + piece64(lane, j));
+                                c0[4 * j] = g.x; c0[4 * j + 1] = g.y; c0[4 * j + 2] = g.z; c0[4 * j + 3] = g.w;
+                                c1[4 * j] = w.x; c1[4 * j + 1] = w.y; c1[4 * j + 2] = w.z; c1[4 * j + 3] = w.w;
+                            }
+                            __syncwarp();  // all have read the buffer before the next copy into it
+                            finish_gradient<P, W>(args, row, col, first, c0, c1);
+                        } else {
+                            float v[W];
+                            if constexpr (EPI == EPI_SCALE) {
+                                scaled(args, row_scale, first, c0, c1, v);
+                                fetch(ch + 2);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < W; ++i) v[i] = __uint_as_float(first[i]);
+                            }
+                            const bool bf16 = EPI == EPI_STORE || args.out_bf16;
+                            if (!args.out_mapped) {
+                                if (row < args.M) {
+                                    if (bf16) store_bf16(static_cast<__nv_bfloat16*>(args.out[which]) + row * args.out_pitch + col, v, args.N - col);
+                                    else store_f32(static_cast<float*>(args.out[which]) + row * args.out_pitch + col, v, args.N - col);
+                                }
+                            } else {
+                                // bfloat16 chunks are 2 KiB, so there are two buffers for them
+                                uint32_t to = slab;
+                                if (bf16) {
+                                    if (lane == 0) tma_store_wait_read<1>();
+                                    to += (uint32_t)z_use * 2048u;
+                                    z_use ^= 1;
+                                } else if (lane == 0) {
+                                    tma_store_wait_read<0>();
+                                }
+                                __syncwarp();
+                                if (bf16) stage_row_bf16(to, lane, v);
+                                else stage_row_f32(to, lane, v);
+                                fence_async_smem();
+                                __syncwarp();
+                                if (lane == 0) {
+                                    tma_store_2d(&maps.out[which], to, col, (int)row0);
+                                    tma_store_commit();
+                                }
+                            }
+                        }
                         __syncwarp();
                     }
+                    if (!ok) break;
                     if (SUBS == 1) acc ^= 1;
                 }
             }
@@ -569,6 +697,12 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 }
             }
         }
+        if (EPI == EPI_GRAD && P == 1)
+            for (; z_out > 0; --z_out) {  // after a time-out: copies in flight land before the shared memory goes away
+                drain(smem_u32(&bar_z[ew * 2 + z_use]), z_phases >> z_use & 1u, args.dev_status);
+                z_use ^= 1;
+            }
+        if (lane == 0) tma_store_wait_all();
         __syncwarp();
     }
 
@@ -642,8 +776,24 @@ tfjsb_status encode(tfjsb_ctx* ctx, CUtensorMap* map, const Operand& o, Kind kin
     return TFJSB_OK;
 }
 
+// Row-major results (or z), copied in chunks of 32 rows.
+tfjsb_status encode_rows(tfjsb_ctx* ctx, CUtensorMap* map, void* base, bool f32, int64_t columns, int64_t rows, int planes, int64_t pitch, int box,
+                         const char* what) {
+    const int size = f32 ? 4 : 2;
+    cuuint64_t dims[3] = {(cuuint64_t)columns, (cuuint64_t)rows, (cuuint64_t)planes};
+    cuuint64_t strides[2] = {(cuuint64_t)(pitch * size), (cuuint64_t)(pitch * rows * size)};
+    cuuint32_t boxes[3] = {(cuuint32_t)box, 32u, 1u}, elem[3] = {1u, 1u, 1u};
+    const CUresult r = ctx->encode_tiled(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, planes > 1 ? 3 : 2, base, dims,
+                                         strides, boxes, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                         box * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+        return fail(ctx, TFJSB_ERR_CUDA, std::string("cuTensorMapEncodeTiled failed for ") + what + " (CUresult " + std::to_string((int)r) + ")");
+    return TFJSB_OK;
+}
+
 template <int CG, int P, int KIND, int EPI, int SUBS = 1>
-cudaError_t launch(const CUtensorMap* maps, const Args& args, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
+cudaError_t launch(const Maps& maps, const Args& args, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
     auto* kernel = &dense_kernel<CG, P, KIND, EPI, SUBS>;
     cudaError_t e = smem_attr_once(reinterpret_cast<const void*>(kernel), tile::SMEM_LIMIT - 2048);
     if (e != cudaSuccess) return e;
@@ -669,12 +819,12 @@ cudaError_t launch(const CUtensorMap* maps, const Args& args, int grid, size_t s
     }
     cfg.attrs = attr;
     cfg.numAttrs = n;
-    e = cudaLaunchKernelEx(&cfg, kernel, maps[0], maps[1], maps[2], args);
+    e = cudaLaunchKernelEx(&cfg, kernel, maps, args);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
 
-cudaError_t launch_wide(const Product& p, const CUtensorMap* maps, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
+cudaError_t launch_wide(const Product& p, const Maps& maps, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
     if (p.kind == KIND_INT8) return launch<2, 1, KIND_INT8, EPI_SCALE, 2>(maps, p.args, grid, smem, s, launches);
     if (p.epilogue == EPI_GATED) return launch<2, 1, KIND_BF16, EPI_GATED, 2>(maps, p.args, grid, smem, s, launches);
     if (p.epilogue == EPI_GRAD) return launch<2, 1, KIND_BF16, EPI_GRAD, 2>(maps, p.args, grid, smem, s, launches);
@@ -682,7 +832,7 @@ cudaError_t launch_wide(const Product& p, const CUtensorMap* maps, int grid, siz
 }
 
 template <int CG>
-cudaError_t launch_any(const Product& p, const CUtensorMap* maps, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
+cudaError_t launch_any(const Product& p, const Maps& maps, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
     if (p.kind == KIND_INT8) return launch<CG, 1, KIND_INT8, EPI_SCALE>(maps, p.args, grid, smem, s, launches);
     if (p.planes == 1) {
         if (p.epilogue == EPI_GATED) return launch<CG, 1, KIND_BF16, EPI_GATED>(maps, p.args, grid, smem, s, launches);
@@ -777,18 +927,23 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     a.dev_status = ctx->dev_status;
     const int own_n = c.block_n / c.cg;
     const int stage_bytes = p.planes * (c.subs * A_BYTES + own_n * 128);
-    int stages = (tile::SMEM_LIMIT - 2048 - 1024) / stage_bytes;
+    const int slabs = 8 * (p.planes == 3 ? 0 : p.epilogue == EPI_GRAD ? SLAB_BYTES<1, EPI_GRAD> : SLAB_BYTES<1, EPI_STORE>);
+    const int stages = (tile::SMEM_LIMIT - 2048 - 1024 - slabs) / stage_bytes;
     a.stages = stages < MAX_STAGES ? stages : MAX_STAGES;
-    const size_t smem = 1024 + (size_t)a.stages * stage_bytes;
-    CUtensorMap maps[3];
+    const size_t smem = 1024 + (size_t)a.stages * stage_bytes + slabs;
+    Maps maps;
     tfjsb_status st;
     const int b_rows = p.epilogue == EPI_GATED ? c.block_n / 2 : own_n;
-    if ((st = encode(ctx, &maps[0], p.a, p.kind, a.M, a.K, a.a_rows, "A")) != TFJSB_OK) return st;
-    if ((st = encode(ctx, &maps[1], p.b[0], p.kind, a.N, a.K, b_rows, "B")) != TFJSB_OK) return st;
-    if (p.b[1].base) {
-        if ((st = encode(ctx, &maps[2], p.b[1], p.kind, a.N, a.K, b_rows, "B")) != TFJSB_OK) return st;
-    } else {
-        maps[2] = maps[1];
+    if ((st = encode(ctx, &maps.a, p.a, p.kind, a.M, a.K, a.a_rows, "A")) != TFJSB_OK) return st;
+    if ((st = encode(ctx, &maps.b[0], p.b[0], p.kind, a.N, a.K, b_rows, "B")) != TFJSB_OK) return st;
+    maps.b[1] = maps.b[0];
+    if (p.b[1].base && (st = encode(ctx, &maps.b[1], p.b[1], p.kind, a.N, a.K, b_rows, "B")) != TFJSB_OK) return st;
+    if (p.planes == 1 && c.splits == 1) {
+        if (a.z && (st = encode_rows(ctx, &maps.z, a.z, true, a.N, a.M, 2, a.z_pitch, 16, "z")) != TFJSB_OK) return st;
+        const bool f32 = p.epilogue == EPI_SCALE && !a.out_bf16;
+        a.out_mapped = (p.epilogue == EPI_STORE || p.epilogue == EPI_SCALE) && a.out_pitch * (f32 ? 4 : 2) % 16 == 0;
+        for (int i = 0; i < a.outputs && a.out_mapped; ++i)
+            if ((st = encode_rows(ctx, &maps.out[i], a.out[i], f32, a.N, a.M, 1, a.out_pitch, 32, "the result")) != TFJSB_OK) return st;
     }
     const int grid = (int)(c.splits > 1 ? tiles * c.splits : (tiles < slots ? tiles : slots) * c.cg);
     const cudaError_t e = c.subs == 2 ? launch_wide(p, maps, grid, smem, s, &ctx->launches)

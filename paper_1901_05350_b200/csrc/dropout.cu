@@ -31,21 +31,38 @@ struct DropoutArgs {
     float scale;
     uint32_t keys[ROUNDS][2];
     uint32_t offset[2];
+    // what the first two rounds make of the offset alone: see philox
+    uint32_t high1, low1, high2, low2;
     // broadcast masks: the dimensions, neighbours of one kind merged, innermost first; a dimension's step in the mask is 0
     // where it is broadcast
     int dims = 0;
     uint64_t extent[4], step[4];
 };
 
+// The four words of a block.  The offset is the same for all, so one product of the first round is worked out before the launch, and so is one of
+// the second where the upper half of the block's index is 0 (SMALL: less than 2^34 elements).  The multiplier that makes 64 bits of 32 is
+// what bounds the kernel next to memory: 18 of them a block instead of 20.
+template <bool SMALL>
 __device__ __forceinline__ void philox(const DropoutArgs& a, uint64_t block, uint32_t (&w)[4]) {
-    uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = a.offset[0], c3 = a.offset[1];
+    const uint64_t first = (uint64_t)(uint32_t)block * MULTIPLIER[0];
+    uint32_t c0 = a.high1, c1 = a.low1, c2 = (uint32_t)(first >> 32) ^ a.offset[1] ^ a.keys[0][1], c3 = (uint32_t)first;
+    if (!SMALL) c0 ^= (uint32_t)(block >> 32);
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-        const uint64_t p0 = (uint64_t)c0 * MULTIPLIER[0], p1 = (uint64_t)c2 * MULTIPLIER[1];
+    for (int r = 1; r < ROUNDS; ++r) {
+        const uint64_t p1 = (uint64_t)c2 * MULTIPLIER[1];
+        uint32_t h0, l0;
+        if (SMALL && r == 1) {
+            h0 = a.high2;
+            l0 = a.low2;
+        } else {
+            const uint64_t p0 = (uint64_t)c0 * MULTIPLIER[0];
+            h0 = (uint32_t)(p0 >> 32);
+            l0 = (uint32_t)p0;
+        }
         c0 = (uint32_t)(p1 >> 32) ^ c1 ^ a.keys[r][0];
-        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ a.keys[r][1];
+        c2 = h0 ^ c3 ^ a.keys[r][1];
         c1 = (uint32_t)p1;
-        c3 = (uint32_t)p0;
+        c3 = l0;
     }
     w[0] = c0; w[1] = c1; w[2] = c2; w[3] = c3;
 }
@@ -66,6 +83,7 @@ __device__ __forceinline__ uint64_t mask_index(const DropoutArgs& a, uint64_t i,
 
 // Eight words of the stream from word m on (m may be "negative": words before the first mean nothing), out of two blocks or,
 // where m is no multiple of four, three.
+template <bool SMALL>
 __device__ __forceinline__ void run_of_words(const DropoutArgs& a, uint64_t m, uint32_t (&w)[8]) {
     uint32_t v[12];
     const uint64_t block = (uint64_t)((int64_t)m >> 2);
@@ -74,7 +92,7 @@ __device__ __forceinline__ void run_of_words(const DropoutArgs& a, uint64_t m, u
     for (int b = 0; b < 3; ++b) {
         if (b == 2 && r == 0) break;
         uint32_t q[4];
-        philox(a, block + b, q);
+        philox<SMALL>(a, block + b, q);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[4 * b + e] = q[e];
     }
@@ -93,11 +111,12 @@ __device__ __forceinline__ void run_of_words(const DropoutArgs& a, uint64_t m, u
 // The words of the `left` (at most eight) elements from i on.
 template <bool BROADCAST, typename I>
 __device__ __forceinline__ void words_of(const DropoutArgs& a, uint64_t i, int left, uint32_t (&w)[8]) {
+    constexpr bool SMALL = sizeof(I) == 4;
     if (!BROADCAST) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             uint32_t q[4];
-            philox(a, (i >> 2) + b, q);
+            philox<SMALL>(a, (i >> 2) + b, q);
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[4 * b + e] = q[e];
         }
@@ -111,12 +130,12 @@ __device__ __forceinline__ void words_of(const DropoutArgs& a, uint64_t i, int l
         uint32_t u[8];
         if (a.step[0] == 0) {
             uint32_t q[4];
-            philox(a, m >> 2, q);
+            philox<SMALL>(a, m >> 2, q);
             const uint32_t v = (m & 2) ? ((m & 1) ? q[3] : q[2]) : ((m & 1) ? q[1] : q[0]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) u[e] = v;
         } else {
-            run_of_words(a, m - (uint64_t)e0, u);
+            run_of_words<SMALL>(a, m - (uint64_t)e0, u);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -167,11 +186,22 @@ __global__ void __launch_bounds__(BLOCK) dropout_kernel(const __grid_constant__ 
     }
 }
 
+template <bool F32, bool BROADCAST, bool RESIDUAL, typename I>
+cudaError_t launch(const DropoutArgs& a, int sm_count, cudaStream_t s) {
+    auto* kernel = &dropout_kernel<F32, BROADCAST, RESIDUAL, I>;
+    // One wave of blocks, so that none is left over for a second.
+    static const int resident = [kernel] {
+        int n = 0;
+        return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, BLOCK, 0) == cudaSuccess && n > 0 ? n : 1;
+    }();
+    const int64_t needed = (a.n + BLOCK * PER_THREAD - 1) / (BLOCK * PER_THREAD), most = (int64_t)sm_count * resident;
+    return launch_k(kernel, dim3((unsigned)(needed < most ? needed : most)), dim3(BLOCK), 0, s, a);
+}
 template <bool F32, bool RESIDUAL>
-cudaError_t launch(const DropoutArgs& a, int blocks, cudaStream_t s) {
-    if (a.dims == 0) return launch_k(dropout_kernel<F32, false, RESIDUAL, uint32_t>, dim3(blocks), dim3(BLOCK), 0, s, a);
-    if (a.n < (1LL << 31)) return launch_k(dropout_kernel<F32, true, RESIDUAL, uint32_t>, dim3(blocks), dim3(BLOCK), 0, s, a);
-    return launch_k(dropout_kernel<F32, true, RESIDUAL, uint64_t>, dim3(blocks), dim3(BLOCK), 0, s, a);
+cudaError_t launch_any(const DropoutArgs& a, int sm_count, cudaStream_t s) {
+    const bool small = a.n < (1LL << 31);
+    if (a.dims == 0) return small ? launch<F32, false, RESIDUAL, uint32_t>(a, sm_count, s) : launch<F32, false, RESIDUAL, uint64_t>(a, sm_count, s);
+    return small ? launch<F32, true, RESIDUAL, uint32_t>(a, sm_count, s) : launch<F32, true, RESIDUAL, uint64_t>(a, sm_count, s);
 }
 
 bool overlaps_partly(const void* a, const void* b, int64_t bytes) {
@@ -217,6 +247,12 @@ tfjsb_status run(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, const char* x
         for (int k = 0; k < 2; ++k) a.keys[r][k] = (uint32_t)(seed >> (32 * k)) + (uint32_t)r * KEY_STEP[k];
     a.offset[0] = (uint32_t)offset;
     a.offset[1] = (uint32_t)(offset >> 32);
+    const uint64_t p1 = (uint64_t)a.offset[0] * MULTIPLIER[1];
+    a.high1 = (uint32_t)(p1 >> 32) ^ a.keys[0][0];
+    a.low1 = (uint32_t)p1;
+    const uint64_t p2 = (uint64_t)a.high1 * MULTIPLIER[0];
+    a.high2 = (uint32_t)(p2 >> 32);
+    a.low2 = (uint32_t)p2;
     if (noise) {
         // dimensions innermost first; those of extent 1 say nothing, neighbours of one kind are one dimension
         uint64_t in_mask = 1;
@@ -234,13 +270,10 @@ tfjsb_status run(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, const char* x
         }
         if (a.dims == 1 && a.step[0] == 1) a.dims = 0;  // nothing is broadcast
     }
-    const int64_t needed = (a.n + BLOCK * PER_THREAD - 1) / (BLOCK * PER_THREAD);
-    const int64_t most = (int64_t)ctx->sm_count * 8;
-    const int blocks = (int)(needed < most ? needed : most);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t e;
-    if (dtype == TFJSB_DTYPE_F32) e = residual ? launch<true, true>(a, blocks, s) : launch<true, false>(a, blocks, s);
-    else e = residual ? launch<false, true>(a, blocks, s) : launch<false, false>(a, blocks, s);
+    if (dtype == TFJSB_DTYPE_F32) e = residual ? launch_any<true, true>(a, ctx->sm_count, s) : launch_any<true, false>(a, ctx->sm_count, s);
+    else e = residual ? launch_any<false, true>(a, ctx->sm_count, s) : launch_any<false, false>(a, ctx->sm_count, s);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "dropout launch");
     ++ctx->launches;
     return TFJSB_OK;

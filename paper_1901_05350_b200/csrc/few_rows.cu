@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(THREADS) few_rows_int8_kernel(const __grid_con
             for (int k = threadIdx.x * 8; k < a.pitch; k += THREADS * 8) {
                 float v[8] = {};
                 if (t < a.rows && k < a.K) values8<QUANTIZE == 2>(a.x, (int64_t)t * a.K + k, a.K - k < 8 ? a.K - k : 8, v);
-                *reinterpret_cast<uint2*>(q + t * a.pitch + k) = quantize8(v, rs);
+                *reinterpret_cast<uint2*>(q + t * a.pitch + k) = quantize8<QUANTIZE == 2>(v, rs);
             }
         }
         __syncthreads();

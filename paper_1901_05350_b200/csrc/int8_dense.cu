@@ -15,30 +15,31 @@ namespace {
 constexpr int64_t MAX_K = 131072;  // 2^17 products of at most 2^14: sums fit 32 bits
 constexpr int QUANTIZE_THREADS = 256;
 
-// A block has a row: its values stay in registers between the maximum and the rounding, up to 4 groups of eight a thread; those
-// of longer rows are read again.
-template <bool F32>
+// A block has a row.  Its first HELD groups of 2048 values stay in registers between the maximum and the rounding, the others are read again.
+template <bool F32, int HELD>
 __global__ void __launch_bounds__(QUANTIZE_THREADS) quantize_kernel(const void* x, int64_t columns, int64_t pitch, int8_t* q, float* scale) {
-    ptx::pdl_launch_dependents();
     ptx::pdl_wait();
+    ptx::pdl_launch_dependents();
     __shared__ float part[QUANTIZE_THREADS / 32];
-    constexpr int HELD = 4, STEP = QUANTIZE_THREADS * 8;
-    const int64_t row = blockIdx.x;
-    const int64_t base = row * columns;
+    constexpr int STEP = QUANTIZE_THREADS * 8;
+    const int64_t row = blockIdx.x, base = row * columns;
+    auto left_at = [&](int64_t c) { return columns - c < 8 ? (int)(columns - c) : 8; };
     float held[HELD][8];
     float amax = 0.f;
 #pragma unroll
     for (int j = 0; j < HELD; ++j) {
         const int64_t c = (int64_t)j * STEP + threadIdx.x * 8;
-        if (c < columns) {
-            values8<F32>(x, base + c, columns - c < 8 ? (int)(columns - c) : 8, held[j]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) amax = max_nan(amax, fabsf(held[j][e]));
-        }
+        for (int e = 0; e < 8; ++e) held[j][e] = 0.f;
+        if (c < columns) values8<F32>(x, base + c, left_at(c), held[j]);
     }
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax = max_nan(amax, fabsf(held[j][e]));
     for (int64_t c = (int64_t)HELD * STEP + threadIdx.x * 8; c < columns; c += STEP) {
         float v[8];
-        values8<F32>(x, base + c, columns - c < 8 ? (int)(columns - c) : 8, v);
+        values8<F32>(x, base + c, left_at(c), v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) amax = max_nan(amax, fabsf(v[e]));
     }
@@ -51,32 +52,27 @@ __global__ void __launch_bounds__(QUANTIZE_THREADS) quantize_kernel(const void* 
     for (int w = 1; w < QUANTIZE_THREADS / 32; ++w) amax = max_nan(amax, part[w]);
     const RowScale r = row_scale(amax);
     if (threadIdx.x == 0) scale[row] = amax / 127.f;
-#pragma unroll 1
-    for (int j = 0; j * (int64_t)STEP < pitch; ++j) {
+    int8_t* out = q + row * pitch;  // the pitch is a multiple of 16
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) {
         const int64_t c = (int64_t)j * STEP + threadIdx.x * 8;
-        if (c >= pitch) break;
-        float v[8];
-        if (j < HELD && c < columns) {
-#pragma unroll
-            for (int k = 0; k < HELD; ++k)
-                if (k == j) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = held[k][e];
-                }
-        } else if (c < columns) {
-            values8<F32>(x, base + c, columns - c < 8 ? (int)(columns - c) : 8, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 0.f;
-        }
-        *reinterpret_cast<uint2*>(q + row * pitch + c) = quantize8(v, r);  // the pitch is a multiple of 16
+        if (c < pitch) *reinterpret_cast<uint2*>(out + c) = quantize8<F32>(held[j], r);
+    }
+    for (int64_t c = (int64_t)HELD * STEP + threadIdx.x * 8; c < pitch; c += STEP) {
+        float v[8] = {};
+        if (c < columns) values8<F32>(x, base + c, left_at(c), v);
+        *reinterpret_cast<uint2*>(out + c) = quantize8<F32>(v, r);
     }
 }
 
-cudaError_t launch_quantize(bool f32, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, cudaStream_t s, int64_t* launches) {
+template <bool F32>
+cudaError_t launch_quantize_as(const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, cudaStream_t s) {
     const int64_t pitch = (columns + 15) / 16 * 16;
-    const cudaError_t e = f32 ? launch_k(quantize_kernel<true>, dim3((unsigned)rows), dim3(QUANTIZE_THREADS), 0, s, x, columns, pitch, q, scale)
-                              : launch_k(quantize_kernel<false>, dim3((unsigned)rows), dim3(QUANTIZE_THREADS), 0, s, x, columns, pitch, q, scale);
+    auto* kernel = columns <= 2048 ? &quantize_kernel<F32, 1> : columns <= 4096 ? &quantize_kernel<F32, 2> : &quantize_kernel<F32, 4>;
+    return launch_k(kernel, dim3((unsigned)rows), dim3(QUANTIZE_THREADS), 0, s, x, columns, pitch, q, scale);
+}
+cudaError_t launch_quantize(bool f32, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, cudaStream_t s, int64_t* launches) {
+    const cudaError_t e = f32 ? launch_quantize_as<true>(x, rows, columns, q, scale, s) : launch_quantize_as<false>(x, rows, columns, q, scale, s);
     if (e == cudaSuccess) ++*launches;
     return e;
 }

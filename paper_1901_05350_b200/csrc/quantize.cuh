@@ -8,8 +8,14 @@ namespace tfjsb {
 namespace dense {
 
 // q = 127 x / amax rounded to nearest, halves to even.  Whether a value lies above, on or below the middle between two integers is decided
-// exactly: 127 |x| is t + t_low (a product and its fma rest), q0 the integer nearest to t / amax as computed, and the sign of
-// 127 |x| - (q0 +- 1/2) amax, of which t - q0 amax is exact (one fma; the terms nearly cancel), settles whether q0 is it.
+// exactly.
+//
+// The quotient r is t / amax with t = 127 x, corrected by its own remainder (an fma), which leaves it within an ulp and exact where it can be: a bfloat16
+// x makes t exact (15 bits), a middle between two integers is representable, and no other quotient comes nearer to one than 2^-8 / 255 of
+// the larger of 1 and its own size, which is more than an ulp.  So for bfloat16 rounding r is right.  For fp32 values t is rounded;
+// there a quotient within 2^-9 of a middle is decided again: 127 |x| is t + t_low (a product and its fma rest), t - q amax
+// is exact for the integer q next to it (one fma, the terms nearly cancel), and the sign of what remains of 127 |x| - (q +- 1/2) amax settles it.
+//
 // Rows of very small or large values are scaled by a power of two first, so that nothing here overflows or loses bits.
 struct RowScale {
     float pre, amax, inverse;  // of pre * x
@@ -23,17 +29,39 @@ __device__ __forceinline__ RowScale row_scale(float amax) {
     r.inverse = 1.f / r.amax;
     return r;
 }
-__device__ __forceinline__ int quantize(float x, const RowScale& r) {
-    if (r.none) return 0;
-    const float v = fabsf(x * r.pre);
+// |x| in [0, 1] times amax: the integer next to 127 |x| / amax
+static __device__ __noinline__ int quantize_near_middle(float x, float pre, float amax, float inverse) {
+    const float v = fabsf(x * pre);
     const float t = v * 127.f, t_low = fmaf(v, 127.f, -t);
-    float q = rintf(t * r.inverse);
-    const float e = fmaf(-q, r.amax, t), middle = 0.5f * r.amax;
+    float q = rintf(t * inverse);
+    const float e = fmaf(-q, amax, t), middle = 0.5f * amax;
     const bool odd = ((int)q & 1) != 0;
     const float above = (e - middle) + t_low, below = (e + middle) + t_low;
     if (above > 0.f || (above == 0.f && odd)) q += 1.f;
     else if (below < 0.f || (below == 0.f && odd)) q -= 1.f;
     return x < 0.f ? -(int)q : (int)q;
+}
+// Eight values as eight bytes.
+template <bool F32>
+__device__ __forceinline__ uint2 quantize8(const float (&v)[8], const RowScale& s) {
+    if (s.none) return make_uint2(0u, 0u);
+    const float c = 127.f * s.pre;
+    uint32_t q[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float t = v[e] * c, r0 = t * s.inverse;
+        const float r = fmaf(fmaf(-r0, s.amax, t), s.inverse, r0);
+        const float m = r + 12582912.f;  // 1.5 * 2^23: the integer nearest to r in the low bits, halves to even
+        q[e] = __float_as_uint(m);
+        if (F32) {
+            const float d = fabsf(r - (m - 12582912.f));
+            if (fabsf(d - 0.5f) < 0.001953125f) q[e] = (uint32_t)quantize_near_middle(v[e], s.pre, s.amax, s.inverse);
+        }
+    }
+    uint2 w;
+    w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+    w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+    return w;
 }
 // The larger of two magnitudes; a NaN wins over all.
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -62,12 +90,6 @@ __device__ __forceinline__ void values8(const void* x, int64_t i, int left, floa
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = e < left ? __uint_as_float((uint32_t)load_global(p + e) << 16) : 0.f;
     }
-}
-__device__ __forceinline__ uint2 quantize8(const float (&v)[8], const RowScale& r) {
-    uint32_t w[2] = {0u, 0u};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e / 4] |= (uint32_t)(quantize(v[e], r) & 0xff) << (e % 4 * 8);
-    return make_uint2(w[0], w[1]);
 }
 
 }  // namespace dense
