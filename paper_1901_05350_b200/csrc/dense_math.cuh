@@ -36,9 +36,20 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& slope) {
         a = relu_nan(g);
         if (SLOPE) slope = g > 0.f ? 1.f : 0.f;
     } else if (GATE == TFJSB_GATE_GELU) {
-        const float f = 0.5f * erfcf(g * -0.70710678118654752f);
+        float f, e;
+        if (EXACT) {
+            f = 0.5f * erfcf(g * -0.70710678118654752f);
+            if (SLOPE) e = expf(-0.5f * g * g);
+        } else {
+            // Abramowitz and Stegun 7.1.26: erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 + p x), off by 1.5e-7 at most; here
+            // x = |g| / sqrt 2 and the coefficients are halved
+            const float t = __fdividef(1.f, fmaf(0.23164189f, fabsf(g), 1.f));
+            e = __expf(-0.5f * g * g);
+            const float tail = t * e * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f);
+            f = g < 0.f ? tail : 1.f - tail;  // a NaN stays one
+        }
         a = g * f;
-        if (SLOPE) slope = f + g * 0.39894228040143268f * (EXACT ? expf(-0.5f * g * g) : __expf(-0.5f * g * g));
+        if (SLOPE) slope = fmaf(g * 0.39894228040143268f, e, f);
     } else {
         const float g2 = g * g;
         const float s = logistic<EXACT>(1.5957691216057308f * g * fmaf(0.044715f, g2, 1.f));

@@ -41,7 +41,8 @@ using tile::drain;
 
 namespace {
 
-constexpr int THREADS = 320;  // producer warp, MMA warp, 8 epilogue warps
+constexpr int THREADS = 352;  // producer warp of A, MMA warp, 8 epilogue warps, producer warp of B
+constexpr int B_WARP = 10;
 constexpr int MAX_STAGES = 8;
 constexpr int ROWS = 128;     // of a CTA's tile
 constexpr int A_BYTES = ROWS * 128;
@@ -87,6 +88,11 @@ __device__ __forceinline__ void load3(uint32_t dst, const CUtensorMap* map, uint
     else tma_load_3d(dst, map, bar, c0, c1, c2);
 }
 
+// Arrival on the even CTA's barrier that orders no memory: what it hands back is tensor memory, whose reads are complete.  One that releases
+// waits for the stores before it, which took 900 cycles.
+__device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 __device__ __forceinline__ uint4 lds4_cluster(uint32_t addr) {
     uint4 v;
     asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
@@ -95,6 +101,28 @@ __device__ __forceinline__ uint4 lds4_cluster(uint32_t addr) {
 
 __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[32]) { tc_ld_32x32(at, r); }
 __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[16]) { tc_ld_cols(at, r); }
+
+// The sum of eight columns' parts, from the shared memory of the cluster's CTAs: all on their way at once (a round trip takes about a
+// microsecond), added in the order of the slices.
+template <int KIND>
+__device__ __forceinline__ void pull_parts(uint32_t at, int splits, uint32_t (&sum)[8]) {
+    uint4 x[8][2];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        if (r < splits) {
+            const uint32_t from = map_to_cta(at, (uint32_t)r);
+            x[r][0] = lds4_cluster(from);
+            x[r][1] = lds4_cluster(from + 16u);
+        }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0u;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        if (r < splits) {
+            add_part<KIND>(sum, 0, x[r][0]);
+            add_part<KIND>(sum, 4, x[r][1]);
+        }
+}
 
 struct Maps {
     CUtensorMap a, b[2];
@@ -225,7 +253,7 @@ __device__ __forceinline__ void finish(const Args& a, int which, int64_t row, in
     }
 }
 
-template <int CG, int P, int KIND, int EPI, int SUBS>
+template <int CG, int P, int KIND, int EPI, int SUBS, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(THREADS, 1)
 dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args args) {
     const CUtensorMap &map_a = maps.a, &map_b0 = maps.b[0], &map_b1 = maps.b[1];
@@ -298,58 +326,71 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
     pdl_launch_dependents();
     pdl_wait();
 
-    if (warp == 0) {
-        // ---------------------------------------------------------------- producer
+    if (warp == 0 || warp == B_WARP) {
+        // ---------------------------------------------------------------- producers: of A (which arms the barriers) and of B
+        // One thread issues a copy in 150 to 250 cycles, so the two operands have a warp each, and everything that an issue takes is
+        // worked out by the whole warp outside the branch (see elect_one).
+        const bool is_a = warp == 0;
         int stage = 0;
         uint32_t phase = 0;
         int issued = 0;
         const bool elected = elect_one();
         bool ok = true;  // the elected thread's
+        constexpr int A_GROUPS = A_MN ? ROWS / 64 : 1, A_COPIES = SUBS * P * A_GROUPS;
+        constexpr int B_MATS = EPI == EPI_GATED && CG == 1 ? 2 : 1, B_GROUPS = B_MN ? 4 / B_MATS / CG : 1, B_COPIES = P * B_MATS * B_GROUPS;
+        const int mat_n = own_n / B_MATS, groups = B_MN ? mat_n / 64 : 1;
         for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
             const Item it = item_at<SUBS>(args, tile);
             const int tn = it.tn;
             const int which = EPI == EPI_STORE && tn >= args.n_tiles ? 1 : 0;
             const int m0 = it.tm * TILE_M + it.sub * (CG * ROWS) + (int)rank * ROWS;
             const int n0 = EPI == EPI_GATED ? tn * (block_n >> 1) : (tn - which * args.n_tiles) * block_n + (int)rank * own_n;
+            const uint32_t tx = (uint32_t)it.subs * a_tx + b_tx;
             for (int kb = kb_begin; kb < kb_end; ++kb) {
-                const int pass = kb / args.num_kb;  // 0 or 1
+                const int pass = kb >= args.num_kb ? 1 : 0;
                 const int k0 = (kb - pass * args.num_kb) * BK;
-                const uint32_t full = CG == 2 ? map_to_cta(smem_u32(&bar_full[stage]), 0u) : smem_u32(&bar_full[stage]);
-                const uint32_t a_dst = stage_base + (uint32_t)stage * stage_bytes, b_dst = a_dst + SUBS * P * a_plane;
-                // the weights of this half of the columns, of this pass, or one and the same
-                const CUtensorMap* map_b = (EPI == EPI_GATED ? (CG == 2 && rank == 1) : pass == 1) ? &map_b1 : &map_b0;
-                if (elected && ok && (ok = bounded_wait(smem_u32(&bar_empty[stage]), phase ^ 1u, abort_flag))) {
-                    if (leader) mbar_arrive_expect_tx(smem_u32(&bar_full[stage]), (uint32_t)it.subs * a_tx + b_tx);
+                const uint32_t own_full = smem_u32(&bar_full[stage]), empty = smem_u32(&bar_empty[stage]);
+                const uint32_t full = CG == 2 ? map_to_cta(own_full, 0u) : own_full;
+                const uint32_t dst = stage_base + (uint32_t)stage * stage_bytes + (is_a ? 0u : SUBS * P * a_plane);
+                if (is_a) {
+                    uint32_t to[A_COPIES];
+                    int c0[A_COPIES], c1[A_COPIES], c2[A_COPIES];
 #pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        const int pa = pass * P + p, pb = which * P + p;
-                        const uint32_t ad = a_dst + p * a_plane, bd = b_dst + p * b_plane;
-                        for (int u = 0; u < (SUBS == 1 ? 1 : it.subs); ++u) {
-                            const int mu = m0 + u * (CG * ROWS);
-                            const uint32_t au = ad + (uint32_t)u * (P * a_plane);
-                            if (args.a_mn) {
-                                for (int i = 0; i < ROWS / 64; ++i) load3<CG>(au + i * GROUP_BYTES, &map_a, full, mu + 64 * i, k0, pa);
-                            } else {
-                                load3<CG>(au, &map_a, full, k0, mu, pa);
-                            }
-                        }
-                        if (EPI == EPI_GATED && CG == 1) {
-                            const int half = own_n >> 1;
-                            for (int w = 0; w < 2; ++w) {
-                                const CUtensorMap* mb = w ? &map_b1 : &map_b0;
-                                if (args.b_mn) {
-                                    for (int i = 0; i < half / 64; ++i) load3<CG>(bd + w * half * 128 + i * GROUP_BYTES, mb, full, n0 + 64 * i, k0, pb);
-                                } else {
-                                    load3<CG>(bd + w * half * 128, mb, full, k0, n0, pb);
-                                }
-                            }
-                        } else if (args.b_mn) {
-                            for (int i = 0; i < own_n / 64; ++i) load3<CG>(bd + i * GROUP_BYTES, map_b, full, n0 + 64 * i, k0, pb);
-                        } else {
-                            load3<CG>(bd, map_b, full, k0, n0, pb);
-                        }
+                    for (int i = 0; i < A_COPIES; ++i) {
+                        const int g = i % A_GROUPS, u = i / A_GROUPS % SUBS, p = i / A_GROUPS / SUBS;
+                        const int row = m0 + u * (CG * ROWS) + 64 * g;
+                        to[i] = dst + (uint32_t)(p * SUBS + u) * a_plane + (uint32_t)g * GROUP_BYTES;
+                        c0[i] = A_MN ? row : k0;
+                        c1[i] = A_MN ? k0 : row;
+                        c2[i] = pass * P + p;
                     }
-                    ++issued;
+                    if (elected && ok && (ok = bounded_wait(empty, phase ^ 1u, abort_flag))) {
+                        if (leader) mbar_arrive_expect_tx(own_full, tx);
+#pragma unroll
+                        for (int i = 0; i < A_COPIES; ++i)
+                            if (SUBS == 1 || i / A_GROUPS % SUBS < it.subs) load3<CG>(to[i], &map_a, full, c0[i], c1[i], c2[i]);
+                        ++issued;
+                    }
+                } else {
+                    // the weights of this half of the columns, of this pass, or one and the same
+                    const CUtensorMap* map_b = (EPI == EPI_GATED ? (CG == 2 && rank == 1) : pass == 1) ? &map_b1 : &map_b0;
+                    uint32_t to[B_COPIES];
+                    int c0[B_COPIES], c1[B_COPIES], c2[B_COPIES];
+#pragma unroll
+                    for (int i = 0; i < B_COPIES; ++i) {
+                        const int g = i % B_GROUPS, w = i / B_GROUPS % B_MATS, p = i / B_GROUPS / B_MATS;
+                        const int row = n0 + 64 * g;
+                        to[i] = dst + (uint32_t)p * b_plane + (uint32_t)(w * mat_n) * 128u + (uint32_t)g * GROUP_BYTES;
+                        c0[i] = B_MN ? row : k0;
+                        c1[i] = B_MN ? k0 : row;
+                        c2[i] = which * P + p;
+                    }
+                    if (elected && ok && (ok = bounded_wait(empty, phase ^ 1u, abort_flag))) {
+#pragma unroll
+                        for (int i = 0; i < B_COPIES; ++i)
+                            if (i % B_GROUPS < groups) load3<CG>(to[i], B_MATS == 2 && i / B_GROUPS % B_MATS ? &map_b1 : map_b, full, c0[i], c1[i], c2[i]);
+                        ++issued;
+                    }
                 }
                 if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
@@ -358,7 +399,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
             give_up(abort_flag, args.dev_status, DEV_STATUS_TIMEOUT_PRODUCER);
             // copies in flight must land before this CTA's shared memory goes away; the odd CTA of a pair has no barrier of
             // its own to watch and waits out the longest that a copy can take
-            if (leader) {
+            if (leader && is_a) {
                 for (int k = (issued > stages ? issued - stages : 0); k < issued; ++k)
                     drain(smem_u32(&bar_full[k % stages]), (uint32_t)((k / stages) & 1), args.dev_status);
             } else {
@@ -373,8 +414,8 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
             const uint32_t formats = KIND == KIND_BF16 ? (1u << 4) | (1u << 7) | (1u << 10)   // fp32 sums of bfloat16
                                                        : (2u << 4) | (1u << 7) | (1u << 10);  // 32-bit sums of signed 8-bit
             const uint32_t idesc = formats | ((uint32_t)(block_n >> 3) << 17) | ((uint32_t)(CG * ROWS >> 4) << 24) |
-                                   (args.a_mn ? IDESC_A_MN : 0u) | (args.b_mn ? IDESC_B_MN : 0u);
-            const uint64_t a_step = args.a_mn ? 128 : 2, b_step = args.b_mn ? 128 : 2;  // of an MMA along K, in 16 bytes
+                                   (A_MN ? IDESC_A_MN : 0u) | (B_MN ? IDESC_B_MN : 0u);
+            constexpr uint64_t a_step = A_MN ? 128 : 2, b_step = B_MN ? 128 : 2;  // of an MMA along K, in 16 bytes
             int stage = 0;
             uint32_t phase = 0;
             int acc = 0;
@@ -391,13 +432,17 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                 auto issue = [&](int at_stage, uint32_t at_phase, int part, bool first, bool wait) {
                     const uint32_t base = stage_base + (uint32_t)at_stage * stage_bytes, a_addr = base + (uint32_t)part * a_plane;
                     const uint32_t b_addr = base + 2 * a_plane;
-                    const uint64_t da = args.a_mn ? mn_desc(a_addr) : make_kmajor_sw128_desc(a_addr);
-                    const uint64_t db = args.b_mn ? mn_desc(b_addr) : make_kmajor_sw128_desc(b_addr);
-                    const uint32_t d = tmem_base + (uint32_t)part * acc_cols;
-                    if (elected && ok && (!wait || (ok = bounded_wait(smem_u32(&bar_full[at_stage]), at_phase, abort_flag)))) {
+                    uint64_t da[4], db[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        da[k] = (A_MN ? mn_desc(a_addr) : make_kmajor_sw128_desc(a_addr)) + a_step * k;
+                        db[k] = (B_MN ? mn_desc(b_addr) : make_kmajor_sw128_desc(b_addr)) + b_step * k;
+                    }
+                    const uint32_t d = tmem_base + (uint32_t)part * acc_cols, full = smem_u32(&bar_full[at_stage]), begun = first ? 0u : 1u;
+                    if (elected && ok && (!wait || (ok = bounded_wait(full, at_phase, abort_flag)))) {
                         if (wait) tc_fence_after();
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) mma<CG, KIND>(d, da + a_step * k, db + b_step * k, idesc, first && k == 0 ? 0u : 1u);
+                        for (int k = 0; k < 4; ++k) mma<CG, KIND>(d, da[k], db[k], idesc, k == 0 ? begun : 1u);
                         issued_any = true;
                     }
                 };
@@ -434,28 +479,31 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                     if (in_segment == 0 && elected && ok) ok = bounded_wait(smem_u32(&bar_acc_empty[acc]), acc_phase ^ 1u, abort_flag);
                     const uint32_t d = tmem_base + (uint32_t)acc * acc_cols;
                     const uint32_t a_addr = stage_base + (uint32_t)stage * stage_bytes, b_addr = a_addr + P * a_plane;
-                    uint64_t da[P], db[P];
+                    uint64_t da[P][4], db[P][4];
 #pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        da[p] = args.a_mn ? mn_desc(a_addr + p * a_plane) : make_kmajor_sw128_desc(a_addr + p * a_plane);
-                        db[p] = args.b_mn ? mn_desc(b_addr + p * b_plane) : make_kmajor_sw128_desc(b_addr + p * b_plane);
-                    }
-                    if (elected && ok && (ok = bounded_wait(smem_u32(&bar_full[stage]), phase, abort_flag))) {
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            da[p][k] = (A_MN ? mn_desc(a_addr + p * a_plane) : make_kmajor_sw128_desc(a_addr + p * a_plane)) + a_step * k;
+                            db[p][k] = (B_MN ? mn_desc(b_addr + p * b_plane) : make_kmajor_sw128_desc(b_addr + p * b_plane)) + b_step * k;
+                        }
+                    const uint32_t begun = in_segment != 0 ? 1u : 0u, full = smem_u32(&bar_full[stage]), empty = smem_u32(&bar_empty[stage]);
+                    const uint32_t small = d + (uint32_t)block_n;
+                    if (elected && ok && (ok = bounded_wait(full, phase, abort_flag))) {
                         tc_fence_after();
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const uint32_t more = (in_segment | k) != 0 ? 1u : 0u;
-                            mma<CG, KIND>(d, da[0] + a_step * k, db[0] + b_step * k, idesc, more);
+                            const uint32_t more = k == 0 ? begun : 1u;
+                            mma<CG, KIND>(d, da[0][k], db[0][k], idesc, more);
                             if constexpr (P == 3) {
-                                const uint32_t small = d + (uint32_t)block_n;
-                                mma<CG, KIND>(small, da[2] + a_step * k, db[0] + b_step * k, idesc, more);
-                                mma<CG, KIND>(small, da[0] + a_step * k, db[2] + b_step * k, idesc, 1u);
-                                mma<CG, KIND>(small, da[1] + a_step * k, db[1] + b_step * k, idesc, 1u);
-                                mma<CG, KIND>(small, da[1] + a_step * k, db[0] + b_step * k, idesc, 1u);
-                                mma<CG, KIND>(small, da[0] + a_step * k, db[1] + b_step * k, idesc, 1u);
+                                mma<CG, KIND>(small, da[2][k], db[0][k], idesc, more);
+                                mma<CG, KIND>(small, da[0][k], db[2][k], idesc, 1u);
+                                mma<CG, KIND>(small, da[1][k], db[1][k], idesc, 1u);
+                                mma<CG, KIND>(small, da[1][k], db[0][k], idesc, 1u);
+                                mma<CG, KIND>(small, da[0][k], db[1][k], idesc, 1u);
                             }
                         }
-                        commit<CG>(smem_u32(&bar_empty[stage]));
+                        commit<CG>(empty);
                         issued_any = true;
                     }
                     if (++stage == stages) { stage = 0; phase ^= 1u; }
@@ -484,6 +532,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
         // took longer than the work.
         constexpr int W = EPI == EPI_GATED || EPI == EPI_GRAD ? 16 : 32;
         const int quad = warp & 3, half = (warp - 2) >> 2;
+        const bool elected = elect_one();  // issues the warp's copies
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const int n_chunks = block_n / W / (EPI == EPI_GATED ? 2 : 1);  // chunks, or pairs of them
         const int segments = P == 3 ? (kb_end - kb_begin + args.seg_kb - 1) / args.seg_kb : 1;
@@ -509,7 +558,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
-                if (CG == 2) mbar_arrive_cluster(map_to_cta(smem_u32(&bar_acc_empty[acc]), 0u));
+                if (CG == 2) arrive_relaxed(map_to_cta(smem_u32(&bar_acc_empty[acc]), 0u));
                 else mbar_arrive(smem_u32(&bar_acc_empty[acc]));
             }
         };
@@ -555,11 +604,12 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                             load_f32(args.bias + col, c1, args.bias ? left : 0);
                         } else if constexpr (EPI == EPI_GRAD) {  // g and u of 32 rows
                             if (ch >= n_chunks || !rows_live || col >= args.N) return;
-                            if (lane == 0) {
-                                const uint32_t bar = smem_u32(&bar_z[ew * 2 + z_fetch]), to = slab + (uint32_t)z_fetch * 4096u;
+                            const uint32_t bar = smem_u32(&bar_z[ew * 2 + z_fetch]), to = slab + (uint32_t)z_fetch * 4096u, to_u = to + 2048u;
+                            const int r0 = (int)row0;
+                            if (elected) {
                                 mbar_arrive_expect_tx(bar, 4096u);
-                                tma_load_3d(to, &maps.z, bar, col, (int)row0, 0);
-                                tma_load_3d(to + 2048u, &maps.z, bar, col, (int)row0, 1);
+                                tma_load_3d(to, &maps.z, bar, col, r0, 0);
+                                tma_load_3d(to_u, &maps.z, bar, col, r0, 1);
                             }
                             z_fetch ^= 1;
                             ++z_out;
@@ -579,15 +629,17 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                         if (!rows_live || col >= args.N) continue;
                         if constexpr (EPI == EPI_GATED) {
                             if (args.z) {
-                                if (lane == 0) tma_store_wait_read<0>();
+                                if (elected) tma_store_wait_read<0>();
                                 __syncwarp();
                                 stage_row(slab, lane, first);
                                 stage_row(slab + 2048u, lane, second);
                                 fence_async_smem();
                                 __syncwarp();
-                                if (lane == 0) {
-                                    tma_store_3d(&maps.z, slab, col, (int)row0, 0);
-                                    tma_store_3d(&maps.z, slab + 2048u, col, (int)row0, 1);
+                                const uint32_t from_u = slab + 2048u;
+                                const int r0 = (int)row0;
+                                if (elected) {
+                                    tma_store_3d(&maps.z, slab, col, r0, 0);
+                                    tma_store_3d(&maps.z, from_u, col, r0, 1);
                                     tma_store_commit();
                                 }
                             }
@@ -616,25 +668,41 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                             float v[W];
                             if constexpr (EPI == EPI_SCALE) {
                                 scaled(args, row_scale, first, c0, c1, v);
-                                fetch(ch + 2);
+                                if (ch + 2 < n_chunks) fetch(ch + 2);
                             } else {
 #pragma unroll
                                 for (int i = 0; i < W; ++i) v[i] = __uint_as_float(first[i]);
                             }
                             const bool bf16 = EPI == EPI_STORE || args.out_bf16;
                             if (!args.out_mapped) {
-                                if (row < args.M) {
-                                    if (bf16) store_bf16(static_cast<__nv_bfloat16*>(args.out[which]) + row * args.out_pitch + col, v, args.N - col);
-                                    else store_f32(static_cast<float*>(args.out[which]) + row * args.out_pitch + col, v, args.N - col);
+                                // rows are no multiple of 16 bytes: a lane has a column of the chunk, row after row
+                                if (bf16) stage_row_bf16(slab, lane, v);
+                                else stage_row_f32(slab, lane, v);
+                                __syncwarp();
+                                const int rows = (int)min((int64_t)32, args.M - row0);
+                                if (col + lane < args.N) {
+                                    const int64_t to = row0 * args.out_pitch + col + lane;
+#pragma unroll 4
+                                    for (int r = 0; r < rows; ++r) {
+                                        if (bf16) {
+                                            unsigned short b;
+                                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(b) : "r"(slab + piece64(r, lane >> 3) + (uint32_t)(lane & 7) * 2u));
+                                            static_cast<unsigned short*>(args.out[which])[to + r * args.out_pitch] = b;
+                                        } else {
+                                            float f;
+                                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(slab + piece128(r, lane >> 2) + (uint32_t)(lane & 3) * 4u));
+                                            static_cast<float*>(args.out[which])[to + r * args.out_pitch] = f;
+                                        }
+                                    }
                                 }
                             } else {
                                 // bfloat16 chunks are 2 KiB, so there are two buffers for them
                                 uint32_t to = slab;
                                 if (bf16) {
-                                    if (lane == 0) tma_store_wait_read<1>();
+                                    if (elected) tma_store_wait_read<1>();
                                     to += (uint32_t)z_use * 2048u;
                                     z_use ^= 1;
-                                } else if (lane == 0) {
+                                } else if (elected) {
                                     tma_store_wait_read<0>();
                                 }
                                 __syncwarp();
@@ -642,8 +710,10 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                                 else stage_row_f32(to, lane, v);
                                 fence_async_smem();
                                 __syncwarp();
-                                if (lane == 0) {
-                                    tma_store_2d(&maps.out[which], to, col, (int)row0);
+                                const CUtensorMap* map_out = &maps.out[which];
+                                const int r0 = (int)row0;
+                                if (elected) {
+                                    tma_store_2d(map_out, to, col, r0);
                                     tma_store_commit();
                                 }
                             }
@@ -657,18 +727,23 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
             if constexpr (P == 3) {
                 if (ok && args.splits == 1) {
                     const int64_t row = m0 + quad * 32 + lane;
-                    const uint32_t(&v0)[32] = reinterpret_cast<const uint32_t(&)[32]>(sum[0]);
-                    const uint32_t(&v1)[32] = reinterpret_cast<const uint32_t(&)[32]>(sum[1]);
-                    // eight columns at a time: 128 registers are taken by the sums and what was read of them
-#pragma unroll
+                    // Eight columns at a time in a rolled loop; the sums move up in their registers instead of being indexed.
+#pragma unroll 1
                     for (int c = 0; c < 32; c += 8) {
-                        const uint32_t(&w0)[8] = reinterpret_cast<const uint32_t(&)[8]>(v0[c]);
-                        const uint32_t(&w1)[8] = reinterpret_cast<const uint32_t(&)[8]>(v1[c]);
+                        uint32_t w0[8], w1[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) { w0[i] = __float_as_uint(sum[0][i]); w1[i] = __float_as_uint(sum[1][i]); }
+#pragma unroll
+                        for (int i = 0; i < 24; ++i) { sum[0][i] = sum[0][i + 8]; sum[1][i] = sum[1][i + 8]; }
                         if (EPI == EPI_GATED) {
                             finish<P, EPI, 8>(args, which, row, n0 + half * 32 + c, w0, w1);
                         } else {
-                            finish<P, EPI, 8>(args, which, row, n0 + half * 32 + c, w0, w0);
-                            finish<P, EPI, 8>(args, which, row, n0 + (half + 2) * 32 + c, w1, w1);
+#pragma unroll 1
+                            for (int j = 0; j < 2; ++j) {
+                                finish<P, EPI, 8>(args, which, row, n0 + (half + 2 * j) * 32 + c, w0, w0);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) w0[i] = w1[i];
+                            }
                         }
                     }
                 }
@@ -702,7 +777,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                 drain(smem_u32(&bar_z[ew * 2 + z_use]), z_phases >> z_use & 1u, args.dev_status);
                 z_use ^= 1;
             }
-        if (lane == 0) tma_store_wait_all();
+        if (elected) tma_store_wait_all();
         __syncwarp();
     }
 
@@ -711,7 +786,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
             cluster_arrive();
             cluster_wait();
             // after a time-out in any CTA the sums are wrong, and the status word says so
-            if (warp >= 2) {
+            if (warp >= 2 && warp < B_WARP) {
                 int tm, tn;
                 tile_at(args, first_tile, &tm, &tn);
                 const int which = EPI == EPI_STORE && tn >= args.n_tiles ? 1 : 0;
@@ -725,20 +800,8 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                     const int row = item / groups, col = (item - row * groups) * 8;
                     const uint32_t at = stage_base + (uint32_t)row * pitch + (uint32_t)col * 4u;
                     uint32_t first[8], second[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) first[i] = second[i] = 0u;
-                    for (int r = 0; r < args.splits; ++r) {
-                        const uint32_t from = map_to_cta(at, (uint32_t)r);
-#pragma unroll
-                        for (int i = 0; i < 8; i += 4) {
-                            const uint4 x = lds4_cluster(from + i * 4u);
-                            add_part<KIND>(first, i, x);
-                            if (EPI == EPI_GATED) {
-                                const uint4 y = lds4_cluster(from + (uint32_t)(columns + i) * 4u);
-                                add_part<KIND>(second, i, y);
-                            }
-                        }
-                    }
+                    pull_parts<KIND>(at, args.splits, first);
+                    if (EPI == EPI_GATED) pull_parts<KIND>(at + (uint32_t)columns * 4u, args.splits, second);
                     finish<P, EPI, 8>(args, which, m0 + row, n0 + col, first, second);
                 }
             }
@@ -792,9 +855,9 @@ tfjsb_status encode_rows(tfjsb_ctx* ctx, CUtensorMap* map, void* base, bool f32,
     return TFJSB_OK;
 }
 
-template <int CG, int P, int KIND, int EPI, int SUBS = 1>
+template <int CG, int P, int KIND, int EPI, int SUBS, bool A_MN, bool B_MN>
 cudaError_t launch(const Maps& maps, const Args& args, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
-    auto* kernel = &dense_kernel<CG, P, KIND, EPI, SUBS>;
+    auto* kernel = &dense_kernel<CG, P, KIND, EPI, SUBS, A_MN, B_MN>;
     cudaError_t e = smem_attr_once(reinterpret_cast<const void*>(kernel), tile::SMEM_LIMIT - 2048);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -824,24 +887,21 @@ cudaError_t launch(const Maps& maps, const Args& args, int grid, size_t smem, cu
     return e;
 }
 
-cudaError_t launch_wide(const Product& p, const Maps& maps, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
-    if (p.kind == KIND_INT8) return launch<2, 1, KIND_INT8, EPI_SCALE, 2>(maps, p.args, grid, smem, s, launches);
-    if (p.epilogue == EPI_GATED) return launch<2, 1, KIND_BF16, EPI_GATED, 2>(maps, p.args, grid, smem, s, launches);
-    if (p.epilogue == EPI_GRAD) return launch<2, 1, KIND_BF16, EPI_GRAD, 2>(maps, p.args, grid, smem, s, launches);
-    return launch<2, 1, KIND_BF16, EPI_STORE, 2>(maps, p.args, grid, smem, s, launches);
-}
-
-template <int CG>
+// The layouts that the layers' products come in: x or h with K contiguous times weights [K, N] (gated, stored), gradients with K
+// contiguous times weights [N, K] (gradient, stored), activations across times gradients across (stored), 8-bit rows.
+template <int CG, int P, int SUBS>
 cudaError_t launch_any(const Product& p, const Maps& maps, int grid, size_t smem, cudaStream_t s, int64_t* launches) {
-    if (p.kind == KIND_INT8) return launch<CG, 1, KIND_INT8, EPI_SCALE>(maps, p.args, grid, smem, s, launches);
-    if (p.planes == 1) {
-        if (p.epilogue == EPI_GATED) return launch<CG, 1, KIND_BF16, EPI_GATED>(maps, p.args, grid, smem, s, launches);
-        if (p.epilogue == EPI_GRAD) return launch<CG, 1, KIND_BF16, EPI_GRAD>(maps, p.args, grid, smem, s, launches);
-        return launch<CG, 1, KIND_BF16, EPI_STORE>(maps, p.args, grid, smem, s, launches);
+    const bool a = p.a.mn, b = p.b[0].mn;
+    if constexpr (P == 1)
+        if (p.kind == KIND_INT8 && !a && !b) return launch<CG, P, KIND_INT8, EPI_SCALE, SUBS, false, false>(maps, p.args, grid, smem, s, launches);
+    if (p.kind == KIND_BF16) {
+        if (p.epilogue == EPI_GATED && !a && b) return launch<CG, P, KIND_BF16, EPI_GATED, SUBS, false, true>(maps, p.args, grid, smem, s, launches);
+        if (p.epilogue == EPI_GRAD && !a && !b) return launch<CG, P, KIND_BF16, EPI_GRAD, SUBS, false, false>(maps, p.args, grid, smem, s, launches);
+        if (p.epilogue == EPI_STORE && !a && b) return launch<CG, P, KIND_BF16, EPI_STORE, SUBS, false, true>(maps, p.args, grid, smem, s, launches);
+        if (p.epilogue == EPI_STORE && !a && !b) return launch<CG, P, KIND_BF16, EPI_STORE, SUBS, false, false>(maps, p.args, grid, smem, s, launches);
+        if (p.epilogue == EPI_STORE && a && b) return launch<CG, P, KIND_BF16, EPI_STORE, SUBS, true, true>(maps, p.args, grid, smem, s, launches);
     }
-    if (p.epilogue == EPI_GATED) return launch<CG, 3, KIND_BF16, EPI_GATED>(maps, p.args, grid, smem, s, launches);
-    if (p.epilogue == EPI_GRAD) return launch<CG, 3, KIND_BF16, EPI_GRAD>(maps, p.args, grid, smem, s, launches);
-    return launch<CG, 3, KIND_BF16, EPI_STORE>(maps, p.args, grid, smem, s, launches);
+    return cudaErrorInvalidValue;
 }
 
 // Which kernel: CTA pairs or single CTAs, columns of a tile, slices of K, parts of a tile's rows.
@@ -852,20 +912,36 @@ int64_t tiles_of(const Product& p, int cg, int block_n, int subs = 1) {
     return ((p.args.M + rows - 1) / rows) * ((p.args.N + columns - 1) / columns) * p.args.outputs;
 }
 
-// Estimated cycles: rounds of tiles x k-blocks x cycles of a k-block, and what a tile and a launch cost beside them.  A k-block's
-// MMAs take 2 cycles a column; single CTAs are bound by their shared memory (operand rows written and read) instead.
+// Estimated cycles, fitted to clocks read in the kernel (at about 1.9 GHz) and to whole products:
+//   - a k-block takes what its MMAs take (2 cycles a column and plane product) or what an SM can fetch (50 bytes a cycle), whichever
+//     is longer; a pair with two parts fetches three tiles for two, a pair half of B, single CTAs everything;
+//   - the first k-block arrives 3400 cycles after the start (4200 in a pair), an epilogue warp takes 900 to 1950 cycles for a chunk;
+//   - with one part a tile the epilogue runs beside the next tile's K loop, with two it holds up the next tile for most of the time it takes;
+//   - slices cost two cluster barriers and a round trip for each share of the tile that a thread adds.
 double cost(const Product& p, const Shape& c, int sm_count) {
-    const int kb = (p.args.K + (p.kind == KIND_BF16 ? 63 : 127)) / (p.kind == KIND_BF16 ? 64 : 128) * p.args.passes;
-    if (c.subs == 2) {
-        const int64_t tiles = tiles_of(p, 2, 256, 2), slots = sm_count / 2, rest = tiles % slots;
-        const double rounds = tiles / slots + (rest == 0 ? 0. : 2 * rest <= slots ? 0.6 : 1.);
-        return rounds * kb * 1150 + 4000;
+    const Args& a = p.args;
+    const int kb = (a.K + (p.kind == KIND_BF16 ? 63 : 127)) / (p.kind == KIND_BF16 ? 64 : 128) * a.passes, own_kb = (kb + c.splits - 1) / c.splits;
+    const double rows = a.M < ROWS ? a.M : ROWS;
+    auto k_block = [&](int subs) {
+        const double fetch = p.planes * 128. * (rows * subs + c.block_n / c.cg) / 50, mma = 2.16 * c.block_n * subs * (p.planes == 3 ? 6 : 1);
+        return fetch > mma ? fetch : mma;
+    };
+    const double main = own_kb * k_block(c.subs), first = c.cg == 2 ? 4200 : 3400;
+    const int columns = p.epilogue == EPI_GATED ? c.block_n / 2 : c.block_n;
+    const double chunk = p.epilogue == EPI_STORE ? 900. / 32 : p.epilogue == EPI_SCALE ? 1200. / 32 : p.epilogue == EPI_GRAD ? 1950. / 16 : a.z ? 1500. / 16 : 1000. / 16;
+    const double epilogue = columns / 2 * chunk * (p.planes == 3 ? 2.5 : 1);
+    const int64_t tiles = tiles_of(p, c.cg, c.block_n, c.subs), slots = sm_count / c.cg;
+    if (c.splits > 1) {
+        const int64_t shares = (int64_t)rows * (columns / 8), each = 256 * c.splits;
+        return first + main + 3200 + (double)((shares + each - 1) / each) * 2000;
     }
-    const double per_kb = (c.cg == 2 ? 2.6 * c.block_n + 20 : 2.0 * c.block_n + 256) * (p.planes == 3 ? 6 : 1);
-    const int64_t tiles = tiles_of(p, c.cg, c.block_n);
-    const int64_t rounds = c.splits > 1 ? 1 : (tiles + sm_count / c.cg - 1) / (sm_count / c.cg);
-    const int own_kb = (kb + c.splits - 1) / c.splits;
-    return (double)rounds * own_kb * per_kb + 10.0 * c.block_n + (c.splits > 1 ? 2500 : 0) + (rounds - 1) * 200;
+    const int64_t rounds = tiles / slots, rest = tiles % slots;
+    if (c.subs == 2) {
+        const double whole = main + 0.8 * epilogue;
+        return first + rounds * whole + (rest == 0 ? 0. : 2 * rest <= slots ? own_kb * k_block(1) + epilogue : whole) + epilogue;
+    }
+    const double step = main > epilogue ? main : epilogue;
+    return first + main + epilogue + (rounds + (rest ? 1 : 0) - 1) * step;
 }
 
 Shape choose(const Product& p, int sm_count) {
@@ -920,8 +996,6 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     }
     a.num_tiles = (int)tiles;
     a.band = 8 / c.subs;
-    a.a_mn = p.a.mn;
-    a.b_mn = p.b[0].mn;
     // of a matrix of less rows than a tile only those are copied (a multiple of 8, the swizzle's period): the others' sums are not stored
     a.a_rows = !p.a.mn && a.M < ROWS ? (a.M + 7) / 8 * 8 : ROWS;
     a.dev_status = ctx->dev_status;
@@ -946,8 +1020,11 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
             if ((st = encode_rows(ctx, &maps.out[i], a.out[i], f32, a.N, a.M, 1, a.out_pitch, 32, "the result")) != TFJSB_OK) return st;
     }
     const int grid = (int)(c.splits > 1 ? tiles * c.splits : (tiles < slots ? tiles : slots) * c.cg);
-    const cudaError_t e = c.subs == 2 ? launch_wide(p, maps, grid, smem, s, &ctx->launches)
-                          : c.cg == 2 ? launch_any<2>(p, maps, grid, smem, s, &ctx->launches) : launch_any<1>(p, maps, grid, smem, s, &ctx->launches);
+    const cudaError_t e = c.subs == 2                      ? launch_any<2, 1, 2>(p, maps, grid, smem, s, &ctx->launches)
+                          : c.cg == 2 && p.planes == 1 ? launch_any<2, 1, 1>(p, maps, grid, smem, s, &ctx->launches)
+                          : c.cg == 2                  ? launch_any<2, 3, 1>(p, maps, grid, smem, s, &ctx->launches)
+                          : p.planes == 1              ? launch_any<1, 1, 1>(p, maps, grid, smem, s, &ctx->launches)
+                                                       : launch_any<1, 3, 1>(p, maps, grid, smem, s, &ctx->launches);
     return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "dense product launch");
 }
 

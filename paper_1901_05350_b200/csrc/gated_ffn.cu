@@ -60,6 +60,7 @@ __global__ void __launch_bounds__(256) layout_kernel(const __grid_constant__ Lay
 
 // ---- layout of the buffers ---------------------------------------------------------------------------------
 constexpr int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
+constexpr int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 constexpr int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
 struct Sizes {
@@ -86,7 +87,7 @@ tfjsb_status sizes_of(const tfjsb_ffn* f, Sizes* s, std::string* why) {
     const bool f32 = f->dtype == TFJSB_DTYPE_F32;
     s->planes = f32 ? 3 : 1;
     s->T = f->tokens; s->D = f->width; s->F = f->hidden; s->Do = f->out_width;
-    s->fp = up8(s->F);
+    s->fp = up16(s->F);  // rows of whole 32-byte sectors
     s->repack_x = f32 || s->D % 8;
     s->repack_up = f32 || s->F % 8;
     s->repack_down = s->repack_dy = f32 || s->Do % 8;
