@@ -37,8 +37,8 @@ struct Args {
     void* out[2] = {nullptr, nullptr};
     int64_t out_pitch = 0, out_plane = 0;  // elements
     int out_mapped = 0;                    // results leave through shared memory
-    float* z = nullptr;                    // [2][M][z_pitch]
-    int64_t z_pitch = 0;
+    float* z = nullptr;                    // g and u in fp32, in blocks of 32 rows x 8 columns: see z_at
+    int64_t z_pitch = 0;                   // columns, a multiple of 8
     int gate = 0;
     int out_bf16 = 1, act = 0;             // EPI_SCALE
     const float *a_scale = nullptr, *b_scale = nullptr, *bias = nullptr;

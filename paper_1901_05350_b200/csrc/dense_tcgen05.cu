@@ -11,7 +11,7 @@
 // gradients of Wg and Wu are one launch over the tiles of both.
 //
 // Structure (CTA pairs, CG = 2, as in gemm_pair.cu; single CTAs, CG = 1, without the cluster): warp 0 copies (TMA), warp 1 issues the
-// MMAs, warps 2-9 are the epilogue, which works on one accumulator stage while the next tile is summed in the other.  The epilogue writes
+// MMAs, warps 2-17 are the epilogue, which works on one accumulator stage while the next tile is summed in the other.  The epilogue writes
 // global memory directly: a thread has a row, 32 bytes of it at a time, so that every sector is written once and whole.
 // Persistent over tiles in bands of `band` tile rows, so that the tiles in flight share operand rows and columns in L2.
 //
@@ -24,6 +24,8 @@
 // additions: the large products go to an accumulator of their own for `seg_kb` k-blocks only (8 additions), the small ones
 // to another, and the epilogue adds both to fp32 sums in registers, rounded to nearest.
 #include <cstdlib>
+#include <map>
+#include <mutex>
 
 #include <cuda_bf16.h>
 
@@ -41,8 +43,9 @@ using tile::drain;
 
 namespace {
 
-constexpr int THREADS = 352;  // producer warp of A, MMA warp, 8 epilogue warps, producer warp of B
-constexpr int B_WARP = 10;
+constexpr int EPI_WARPS = 16;  // four for each quadrant of tensor-memory lanes
+constexpr int B_WARP = 2 + EPI_WARPS;
+constexpr int THREADS = 32 * (B_WARP + 1);  // producer warp of A, MMA warp, epilogue warps, producer warp of B
 constexpr int MAX_STAGES = 8;
 constexpr int ROWS = 128;     // of a CTA's tile
 constexpr int A_BYTES = ROWS * 128;
@@ -101,59 +104,54 @@ __device__ __forceinline__ uint4 lds4_cluster(uint32_t addr) {
 
 __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[32]) { tc_ld_32x32(at, r); }
 __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[16]) { tc_ld_cols(at, r); }
+__device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[8]) { tc_ld_cols(at, r); }
 
-// The sum of eight columns' parts, from the shared memory of the cluster's CTAs: all on their way at once (a round trip takes about a
-// microsecond), added in the order of the slices.
+// The sum of eight columns' parts, from the shared memory of the cluster's CTAs: those of four slices on their way at once (a round trip
+// takes about half a microsecond), added in the order of the slices.
 template <int KIND>
 __device__ __forceinline__ void pull_parts(uint32_t at, int splits, uint32_t (&sum)[8]) {
-    uint4 x[8][2];
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-        if (r < splits) {
-            const uint32_t from = map_to_cta(at, (uint32_t)r);
-            x[r][0] = lds4_cluster(from);
-            x[r][1] = lds4_cluster(from + 16u);
-        }
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0u;
+#pragma unroll 1
+    for (int r = 0; r < splits; r += 4) {
+        uint4 x[4][2];
 #pragma unroll
-    for (int r = 0; r < 8; ++r)
-        if (r < splits) {
-            add_part<KIND>(sum, 0, x[r][0]);
-            add_part<KIND>(sum, 4, x[r][1]);
-        }
+        for (int j = 0; j < 4; ++j)
+            if (r + j < splits) {
+                const uint32_t from = map_to_cta(at, (uint32_t)(r + j));
+                x[j][0] = lds4_cluster(from);
+                x[j][1] = lds4_cluster(from + 16u);
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (r + j < splits) {
+                add_part<KIND>(sum, 0, x[j][0]);
+                add_part<KIND>(sum, 4, x[j][1]);
+            }
+    }
 }
 
 struct Maps {
     CUtensorMap a, b[2];
     CUtensorMap out[2];  // results that are stored from shared memory
-    CUtensorMap z;
 };
 
-// Shared memory of an epilogue warp: chunks of 32 rows on their way out, or of g and u on their way in (two buffers).
-template <int P, int EPI> constexpr int SLAB_BYTES = P == 3 ? 0 : EPI == EPI_GRAD ? 8192 : 4096;
+// Shared memory of an epilogue warp: a chunk of 32 rows of a result on its way out, rows of 64 bytes.
+template <int P, int EPI> constexpr int SLAB_BYTES = P == 1 && (EPI == EPI_STORE || EPI == EPI_SCALE) ? 2048 : 0;
 
-// 16-byte piece j of row r of a chunk whose rows are 64 bytes in the 64-byte swizzle, or 128 bytes in the 128-byte one.
-__device__ __forceinline__ uint32_t piece64(int r, int j) { return (uint32_t)(r * 64 + ((j ^ (r >> 1 & 3)) << 4)); }
-__device__ __forceinline__ uint32_t piece128(int r, int j) { return (uint32_t)(r * 128 + ((j ^ (r & 7)) << 4)); }
+// 16-byte piece j of row r of a chunk whose rows are B bytes, in the swizzle of B bytes.
+template <int B>
+__device__ __forceinline__ uint32_t piece(int r, int j) {
+    return (uint32_t)(r * B + ((j ^ (B == 32 ? r >> 2 & 1 : B == 64 ? r >> 1 & 3 : r & 7)) << 4));
+}
 __device__ __forceinline__ void sts16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-// A row of 16 or 32 fp32 values, or of 32 that are rounded to bfloat16, into the slab.
-__device__ __forceinline__ void stage_row(uint32_t slab, int r, const uint32_t (&v)[16]) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sts16(slab + piece64(r, j), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-}
-__device__ __forceinline__ void stage_row_f32(uint32_t slab, int r, const float (&v)[32]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        sts16(slab + piece128(r, j), __float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
-}
-__device__ __forceinline__ void stage_row_bf16(uint32_t slab, int r, const float (&v)[32]) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        sts16(slab + piece64(r, j), pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]), pack_bf16(v[8 * j + 4], v[8 * j + 5]),
-              pack_bf16(v[8 * j + 6], v[8 * j + 7]));
+
+// Where eight values of g (plane 0) or u of row `row` from column `col` on, a multiple of eight, are in z.  Neighbouring rows' eights are
+// neighbours, in blocks of 32 rows, so that a warp whose lanes have a row each reads or writes 1 KiB in one piece.
+__device__ __forceinline__ float* z_at(const Args& a, int64_t row, int col, int plane) {
+    return a.z + (((row >> 5) * (a.z_pitch >> 3) + (col >> 3)) * 2 + plane) * 256 + (row & 31) * 8;
 }
 
 // Tile number -> (tile row, tile column), in bands of `band` tile rows, down a band's columns one after the other.
@@ -237,18 +235,16 @@ __device__ __forceinline__ void finish(const Args& a, int which, int64_t row, in
         float g[W], u[W];
 #pragma unroll
         for (int i = 0; i < W; ++i) { g[i] = __uint_as_float(first[i]); u[i] = __uint_as_float(second[i]); }
-        if (a.z && (P == 3 || W == 8)) {  // otherwise copied from shared memory
-            float* z = a.z + row * a.z_pitch + col;
-            store_f32(z, g, left);
-            store_f32(z + (int64_t)a.M * a.z_pitch, u, left);
+        if (a.z) {
+            store_f32(z_at(a, row, col, 0), g, W);
+            store_f32(z_at(a, row, col, 1), u, W);
         }
         gated<P == 3>(a.gate, g, u, v);
         store_planes<P>(static_cast<__nv_bfloat16*>(a.out[0]) + row * a.out_pitch + col, a.out_plane, v, left);
     } else {
         float g[W], u[W];
-        const float* z = a.z + row * a.z_pitch + col;
-        load_f32(z, g, left);
-        load_f32(z + (int64_t)a.M * a.z_pitch, u, left);
+        load_f32(z_at(a, row, col, 0), g, W);
+        load_f32(z_at(a, row, col, 1), u, W);
         finish_gradient<P, W>(a, row, col, first, g, u);
     }
 }
@@ -264,7 +260,6 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
     __shared__ __align__(8) uint64_t bar_acc_empty[2];      // CG = 2: used in the even CTA only
     __shared__ __align__(8) uint64_t bar_drain;
     constexpr int SLAB = SLAB_BYTES<P, EPI>;
-    __shared__ __align__(8) uint64_t bar_z[EPI == EPI_GRAD && P == 1 ? 16 : 1];  // of an epilogue warp's two buffers
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag_s;
 
@@ -295,11 +290,9 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_u32(&bar_acc_full[s]), 1);
-            mbar_init(smem_u32(&bar_acc_empty[s]), 8 * CG);  // the epilogue warps
+            mbar_init(smem_u32(&bar_acc_empty[s]), EPI_WARPS * CG);
         }
         mbar_init(smem_u32(&bar_drain), 1);
-        if (EPI == EPI_GRAD && P == 1)
-            for (int i = 0; i < 16; ++i) mbar_init(smem_u32(&bar_z[i]), 1);
         abort_flag_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
@@ -526,21 +519,21 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
         }
         __syncwarp();
     } else {
-        // ---------------------------------------------------------------- epilogue (warps 2..9)
-        // Two warps for each quadrant of tensor-memory lanes (32 rows) take alternate chunks of W columns; a gated tile's chunks
-        // are pairs, of g and of u.  The loop over chunks is rolled: a short call runs its code once, and fetching it unrolled
-        // took longer than the work.
-        constexpr int W = EPI == EPI_GATED || EPI == EPI_GRAD ? 16 : 32;
-        const int quad = warp & 3, half = (warp - 2) >> 2;
+        // ---------------------------------------------------------------- epilogue (warps 2..17)
+        // The four warps of a quadrant of tensor-memory lanes (32 rows) take the chunks of 16 or 32 columns in turn; a gated tile's chunks
+        // are pairs, of g and of u.  What a chunk takes is mostly latency (reading tensor memory 105 cycles, a copy's issue
+        // 150, its buffer being read 230, the gate 400), so there are many warps.  The loop over chunks is rolled: a
+        // short call runs its code once, and fetching it unrolled takes longer than the work.
+        constexpr int PARTS = EPI_WARPS / 4;
+        const int quad = warp & 3, part = (warp - 2) >> 2;
         const bool elected = elect_one();  // issues the warp's copies
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const int n_chunks = block_n / W / (EPI == EPI_GATED ? 2 : 1);  // chunks, or pairs of them
+        const int chunk = EPI == EPI_STORE || (EPI == EPI_SCALE && args.out_bf16) ? 32 : 16;  // columns
+        const int n_chunks = block_n / chunk / (EPI == EPI_GATED ? 2 : 1);  // chunks, or pairs of them
         const int segments = P == 3 ? (kb_end - kb_begin + args.seg_kb - 1) / args.seg_kb : 1;
         const uint32_t pitch = (uint32_t)(block_n + 4) * 4u;  // of a partial tile's row: consecutive rows start 4 banks apart
         const int ew = warp - 2;
         const uint32_t slab = stage_base + (uint32_t)stages * stage_bytes + (uint32_t)(ew * SLAB);
-        int z_fetch = 0, z_use = 0, z_out = 0;  // buffers of the slab, copies in flight
-        uint32_t z_phases = 0;
         int acc = 0;
         uint32_t phases = 0;  // of the accumulators, a bit each
         bool ok = true;
@@ -568,21 +561,20 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
             const int which = EPI == EPI_STORE && tn >= args.n_tiles ? 1 : 0;
             const int64_t m0 = (int64_t)it.tm * TILE_M + it.sub * (CG * ROWS) + (int)rank * ROWS;
             const int n0 = EPI == EPI_GATED ? tn * (block_n >> 1) : (tn - which * args.n_tiles) * block_n;
-            float sum[P == 3 ? 2 : 1][32];  // P = 3: block_n is 128, a warp has two chunks of 32
+            float sum[P == 3 ? 2 : 1][16];  // P = 3: block_n is 128, a warp has two chunks of 16
             if constexpr (P == 3) {
                 for (int segment = 0; segment < segments; ++segment) {
                     if (!(ok = wait_acc())) break;
                     const uint32_t at = tmem_base + lanes + (uint32_t)acc * acc_cols;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        uint32_t large[32];
+                        uint32_t small[16], large[16];
+                        ld_columns(at + (uint32_t)((part + PARTS * j) * 16 + block_n), small);
+                        ld_columns(at + (uint32_t)((part + PARTS * j) * 16), large);
+                        tc_ld_wait();
 #pragma unroll
-                        for (int part = 0; part < 2; ++part) {  // the small products first
-                            tc_ld_32x32(at + (uint32_t)((half + 2 * j) * 32 + (part ? 0 : block_n)), large);
-                            tc_ld_wait();
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) sum[j][i] = (segment | part ? sum[j][i] : 0.f) + __uint_as_float(large[i]);
-                        }
+                        for (int i = 0; i < 16; ++i)
+                            sum[j][i] = ((segment ? sum[j][i] : 0.f) + __uint_as_float(small[i])) + __uint_as_float(large[i]);
                     }
                     release_acc();
                     acc ^= 1;
@@ -594,127 +586,129 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                     if (SUBS == 2) acc = u;
                     const int64_t row0 = m0 + u * (CG * ROWS) + quad * 32, row = row0 + lane;
                     const bool rows_live = row0 < args.M;
-                    float c0[W], c1[W];  // EPI_SCALE: scales and biases of the next chunk's columns, on their way while a chunk is worked on
                     const float row_scale = EPI == EPI_SCALE && row < args.M ? load_global(args.a_scale + row) : 0.f;
-                    auto fetch = [&](int ch) {
-                        const int col = n0 + ch * W;
-                        if constexpr (EPI == EPI_SCALE) {
-                            const int left = ch < n_chunks ? args.N - col : 0;
-                            load_f32(args.b_scale + col, c0, left);
-                            load_f32(args.bias + col, c1, args.bias ? left : 0);
-                        } else if constexpr (EPI == EPI_GRAD) {  // g and u of 32 rows
-                            if (ch >= n_chunks || !rows_live || col >= args.N) return;
-                            const uint32_t bar = smem_u32(&bar_z[ew * 2 + z_fetch]), to = slab + (uint32_t)z_fetch * 4096u, to_u = to + 2048u;
-                            const int r0 = (int)row0;
-                            if (elected) {
-                                mbar_arrive_expect_tx(bar, 4096u);
-                                tma_load_3d(to, &maps.z, bar, col, r0, 0);
-                                tma_load_3d(to_u, &maps.z, bar, col, r0, 1);
-                            }
-                            z_fetch ^= 1;
-                            ++z_out;
+                    float g8[8], u8[8];  // EPI_GRAD: g and u of the next eight columns, on their way while eight are worked on
+                    auto fetch = [&](int col) {
+                        if (EPI == EPI_GRAD && rows_live && col < args.N) {  // rows are filled up to whole blocks
+                            load_f32(z_at(args, row, col, 0), g8, 8);
+                            load_f32(z_at(args, row, col, 1), u8, 8);
                         }
                     };
-                    fetch(half);
+                    if (part < n_chunks) fetch(n0 + part * chunk);
                     if (!(ok = wait_acc())) break;
+                    if (part >= n_chunks) release_acc();
                     const uint32_t at = tmem_base + lanes + (uint32_t)acc * acc_cols;
 #pragma unroll 1
-                    for (int ch = half; ch < n_chunks; ch += 2) {
-                        const int col = n0 + ch * W;
-                        uint32_t first[W], second[EPI == EPI_GATED ? W : 1];
-                        ld_columns(at + (uint32_t)(ch * W), first);
-                        if constexpr (EPI == EPI_GATED) ld_columns(at + (uint32_t)(block_n / 2 + ch * W), second);
-                        tc_ld_wait();
-                        if (ch + 2 >= n_chunks) release_acc();
-                        if (!rows_live || col >= args.N) continue;
-                        if constexpr (EPI == EPI_GATED) {
-                            if (args.z) {
-                                if (elected) tma_store_wait_read<0>();
-                                __syncwarp();
-                                stage_row(slab, lane, first);
-                                stage_row(slab + 2048u, lane, second);
-                                fence_async_smem();
-                                __syncwarp();
-                                const uint32_t from_u = slab + 2048u;
-                                const int r0 = (int)row0;
-                                if (elected) {
-                                    tma_store_3d(&maps.z, slab, col, r0, 0);
-                                    tma_store_3d(&maps.z, from_u, col, r0, 1);
-                                    tma_store_commit();
-                                }
-                            }
-                            finish<P, EPI, W>(args, which, row, col, first, second);
-                        } else if constexpr (EPI == EPI_GRAD) {
-                            fetch(ch + 2);
-                            const bool got = bounded_wait(smem_u32(&bar_z[ew * 2 + z_use]), z_phases >> z_use & 1u, abort_flag);
-                            if (!__all_sync(0xffffffffu, got)) {
-                                if (lane == 0) give_up(abort_flag, args.dev_status, DEV_STATUS_TIMEOUT_EPILOGUE);
-                                ok = false;
-                                break;
-                            }
-                            z_phases ^= 1u << z_use;
-                            --z_out;
-                            const uint32_t from = slab + (uint32_t)z_use * 4096u;
-                            z_use ^= 1;
+                    for (int ch = part; ch < n_chunks; ch += PARTS) {
+                        const int col = n0 + ch * chunk;
+                        if constexpr (EPI == EPI_GATED || EPI == EPI_GRAD) {
+                            uint32_t first[2][8], second[2][8];
 #pragma unroll
-                            for (int j = 0; j < W / 4; ++j) {
-                                const float4 g = tile::lds4(from + piece64(lane, j)), w = tile::lds4(from + 2048u + piece64(lane, j));
-                                c0[4 * j] = g.x; c0[4 * j + 1] = g.y; c0[4 * j + 2] = g.z; c0[4 * j + 3] = g.w;
-                                c1[4 * j] = w.x; c1[4 * j + 1] = w.y; c1[4 * j + 2] = w.z; c1[4 * j + 3] = w.w;
+                            for (int j = 0; j < 2; ++j) {
+                                ld_columns(at + (uint32_t)(ch * 16 + j * 8), first[j]);
+                                if (EPI == EPI_GATED) ld_columns(at + (uint32_t)(block_n / 2 + ch * 16 + j * 8), second[j]);
                             }
-                            __syncwarp();  // all have read the buffer before the next copy into it
-                            finish_gradient<P, W>(args, row, col, first, c0, c1);
-                        } else {
-                            float v[W];
-                            if constexpr (EPI == EPI_SCALE) {
-                                scaled(args, row_scale, first, c0, c1, v);
-                                if (ch + 2 < n_chunks) fetch(ch + 2);
-                            } else {
+                            tc_ld_wait();
+                            if (ch + PARTS >= n_chunks) release_acc();
+                            if (!rows_live || col >= args.N) continue;
+                            float out[EPI == EPI_GATED ? 1 : 2][16];
 #pragma unroll
-                                for (int i = 0; i < W; ++i) v[i] = __uint_as_float(first[i]);
-                            }
-                            const bool bf16 = EPI == EPI_STORE || args.out_bf16;
-                            if (!args.out_mapped) {
-                                // rows are no multiple of 16 bytes: a lane has a column of the chunk, row after row
-                                if (bf16) stage_row_bf16(slab, lane, v);
-                                else stage_row_f32(slab, lane, v);
-                                __syncwarp();
-                                const int rows = (int)min((int64_t)32, args.M - row0);
-                                if (col + lane < args.N) {
-                                    const int64_t to = row0 * args.out_pitch + col + lane;
-#pragma unroll 4
-                                    for (int r = 0; r < rows; ++r) {
-                                        if (bf16) {
-                                            unsigned short b;
-                                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(b) : "r"(slab + piece64(r, lane >> 3) + (uint32_t)(lane & 7) * 2u));
-                                            static_cast<unsigned short*>(args.out[which])[to + r * args.out_pitch] = b;
-                                        } else {
-                                            float f;
-                                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(slab + piece128(r, lane >> 2) + (uint32_t)(lane & 3) * 4u));
-                                            static_cast<float*>(args.out[which])[to + r * args.out_pitch] = f;
-                                        }
+                            for (int j = 0; j < 2; ++j) {
+                                float v[8], w[8], x[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(first[j][i]);
+                                if constexpr (EPI == EPI_GATED) {
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) w[i] = __uint_as_float(second[j][i]);
+                                    if (args.z && col + 8 * j < args.N) {
+                                        store_f32(z_at(args, row, col + 8 * j, 0), v, 8);
+                                        store_f32(z_at(args, row, col + 8 * j, 1), w, 8);
                                     }
+                                    gated<false>(args.gate, v, w, x);
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) out[0][8 * j + i] = x[i];
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) { w[i] = g8[i]; x[i] = u8[i]; }
+                                    const int next = j == 0 ? col + 8 : ch + PARTS < n_chunks ? col + PARTS * 16 : args.N;
+                                    fetch(next);
+                                    float du[8];
+                                    gated_gradient<false>(args.gate, w, x, v, du);
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) { out[0][8 * j + i] = v[i]; out[EPI == EPI_GRAD ? 1 : 0][8 * j + i] = du[i]; }
                                 }
-                            } else {
-                                // bfloat16 chunks are 2 KiB, so there are two buffers for them
-                                uint32_t to = slab;
+                            }
+                            if (row < args.M) {
+                                __nv_bfloat16* to = static_cast<__nv_bfloat16*>(args.out[0]) + row * args.out_pitch + col;
+                                store_bf16(to, out[0], args.N - col);
+                                if (EPI == EPI_GRAD) store_bf16(to + args.out_plane, out[EPI == EPI_GRAD ? 1 : 0], args.N - col);
+                            }
+                        } else {
+                            // rounded (and scaled) values of 32 rows through the slab, eight columns after eight
+                            const bool bf16 = EPI == EPI_STORE || args.out_bf16;
+                            uint32_t sums[4][8];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                if (EPI == EPI_STORE || j * 8 < chunk) ld_columns(at + (uint32_t)(ch * chunk + j * 8), sums[j]);
+                            if (elected) tma_store_wait_read<0>();
+                            tc_ld_wait();
+                            if (ch + PARTS >= n_chunks) release_acc();
+                            if (!rows_live || col >= args.N) continue;
+                            __syncwarp();
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if (EPI == EPI_SCALE && j * 8 >= chunk) break;
+                                float v[8];
+                                if constexpr (EPI == EPI_SCALE) {
+                                    float scale[8], bias[8];
+                                    const int left = args.N - col - 8 * j;
+                                    load_f32(args.b_scale + col + 8 * j, scale, left);
+                                    if (args.bias) load_f32(args.bias + col + 8 * j, bias, left);
+                                    else
+#pragma unroll
+                                        for (int i = 0; i < 8; ++i) bias[i] = 0.f;
+                                    scaled(args, row_scale, sums[j], scale, bias, v);
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(sums[j][i]);
+                                }
                                 if (bf16) {
-                                    if (elected) tma_store_wait_read<1>();
-                                    to += (uint32_t)z_use * 2048u;
-                                    z_use ^= 1;
-                                } else if (elected) {
-                                    tma_store_wait_read<0>();
+                                    sts16(slab + piece<64>(lane, j), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i)
+                                        sts16(slab + piece<64>(lane, 2 * j + i), __float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                                              __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
                                 }
-                                __syncwarp();
-                                if (bf16) stage_row_bf16(to, lane, v);
-                                else stage_row_f32(to, lane, v);
+                            }
+                            if (args.out_mapped) {
                                 fence_async_smem();
                                 __syncwarp();
                                 const CUtensorMap* map_out = &maps.out[which];
                                 const int r0 = (int)row0;
                                 if (elected) {
-                                    tma_store_2d(map_out, to, col, r0);
+                                    tma_store_2d(map_out, slab, col, r0);
                                     tma_store_commit();
+                                }
+                            } else {
+                                // rows are no multiple of 16 bytes: a lane has a column of the chunk, row after row
+                                __syncwarp();
+                                const int rows = (int)min((int64_t)32, args.M - row0), c = lane & (chunk - 1), size = bf16 ? 2 : 4;
+                                if (col + c < args.N) {
+                                    const int64_t to = row0 * args.out_pitch + col + c;
+#pragma unroll 4
+                                    for (int r = lane / chunk; r < rows; r += 32 / chunk) {
+                                        const uint32_t from = slab + piece<64>(r, c * size >> 4) + (uint32_t)(c * size & 15);
+                                        if (bf16) {
+                                            unsigned short b;
+                                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(b) : "r"(from));
+                                            static_cast<unsigned short*>(args.out[which])[to + r * args.out_pitch] = b;
+                                        } else {
+                                            float f;
+                                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(from));
+                                            static_cast<float*>(args.out[which])[to + r * args.out_pitch] = f;
+                                        }
+                                    }
                                 }
                             }
                         }
@@ -729,18 +723,18 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                     const int64_t row = m0 + quad * 32 + lane;
                     // Eight columns at a time in a rolled loop; the sums move up in their registers instead of being indexed.
 #pragma unroll 1
-                    for (int c = 0; c < 32; c += 8) {
+                    for (int c = 0; c < 16; c += 8) {
                         uint32_t w0[8], w1[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) { w0[i] = __float_as_uint(sum[0][i]); w1[i] = __float_as_uint(sum[1][i]); }
 #pragma unroll
-                        for (int i = 0; i < 24; ++i) { sum[0][i] = sum[0][i + 8]; sum[1][i] = sum[1][i + 8]; }
+                        for (int i = 0; i < 8; ++i) { sum[0][i] = sum[0][i + 8]; sum[1][i] = sum[1][i + 8]; }
                         if (EPI == EPI_GATED) {
-                            finish<P, EPI, 8>(args, which, row, n0 + half * 32 + c, w0, w1);
+                            finish<P, EPI, 8>(args, which, row, n0 + part * 16 + c, w0, w1);
                         } else {
 #pragma unroll 1
                             for (int j = 0; j < 2; ++j) {
-                                finish<P, EPI, 8>(args, which, row, n0 + (half + 2 * j) * 32 + c, w0, w0);
+                                finish<P, EPI, 8>(args, which, row, n0 + (part + PARTS * j) * 16 + c, w0, w0);
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) w0[i] = w1[i];
                             }
@@ -753,30 +747,25 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                     // every MMA of this CTA has finished, so the stages' shared memory is free for the partial tile
                     const uint32_t row_at = stage_base + (uint32_t)(quad * 32 + lane) * pitch;
                     if (ok && m0 + quad * 32 < args.M) {
-                        for (int j = 0; half + 2 * j < block_n / 32; ++j) {
-                            const int ch = half + 2 * j;
-                            uint32_t v[32];
+                        // 16 columns at a time
+#pragma unroll 1
+                        for (int j = 0; part + PARTS * j < block_n / 16; ++j) {
+                            const int ch = part + PARTS * j;
+                            uint32_t v[16];
                             if constexpr (P == 3) {
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(j == 0 ? sum[0][i] : sum[1][i]);
+                                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(j == 0 ? sum[0][i] : sum[1][i]);
                             } else {
-                                tc_ld_32x32(tmem_base + lanes + (uint32_t)ch * 32u, v);
+                                ld_columns(tmem_base + lanes + (uint32_t)ch * 16u, v);
                                 tc_ld_wait();
                             }
 #pragma unroll
-                            for (int i = 0; i < 32; i += 4)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row_at + (uint32_t)(ch * 32 + i) * 4u), "r"(v[i]),
-                                             "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]) : "memory");
+                            for (int i = 0; i < 16; i += 4) sts16(row_at + (uint32_t)(ch * 16 + i) * 4u, v[i], v[i + 1], v[i + 2], v[i + 3]);
                         }
                     }
                 }
             }
         }
-        if (EPI == EPI_GRAD && P == 1)
-            for (; z_out > 0; --z_out) {  // after a time-out: copies in flight land before the shared memory goes away
-                drain(smem_u32(&bar_z[ew * 2 + z_use]), z_phases >> z_use & 1u, args.dev_status);
-                z_use ^= 1;
-            }
         if (elected) tma_store_wait_all();
         __syncwarp();
     }
@@ -796,7 +785,8 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                 const int groups = columns / 8;
                 const int rows = (int)min((int64_t)ROWS, args.M - m0);
                 const uint32_t pitch = (uint32_t)(block_n + 4) * 4u;
-                for (int item = (int)slice * 256 + (int)threadIdx.x - 64; item < rows * groups; item += 256 * args.splits) {
+                constexpr int WORKERS = 32 * EPI_WARPS;
+                for (int item = (int)slice * WORKERS + (int)threadIdx.x - 64; item < rows * groups; item += WORKERS * args.splits) {
                     const int row = item / groups, col = (item - row * groups) * 8;
                     const uint32_t at = stage_base + (uint32_t)row * pitch + (uint32_t)col * 4u;
                     uint32_t first[8], second[8];
@@ -839,19 +829,16 @@ tfjsb_status encode(tfjsb_ctx* ctx, CUtensorMap* map, const Operand& o, Kind kin
     return TFJSB_OK;
 }
 
-// Row-major results (or z), copied in chunks of 32 rows.
-tfjsb_status encode_rows(tfjsb_ctx* ctx, CUtensorMap* map, void* base, bool f32, int64_t columns, int64_t rows, int planes, int64_t pitch, int box,
-                         const char* what) {
+// A row-major result, stored in chunks of 32 rows of 64 bytes.
+tfjsb_status encode_result(tfjsb_ctx* ctx, CUtensorMap* map, void* base, bool f32, int64_t columns, int64_t rows, int64_t pitch) {
     const int size = f32 ? 4 : 2;
-    cuuint64_t dims[3] = {(cuuint64_t)columns, (cuuint64_t)rows, (cuuint64_t)planes};
-    cuuint64_t strides[2] = {(cuuint64_t)(pitch * size), (cuuint64_t)(pitch * rows * size)};
-    cuuint32_t boxes[3] = {(cuuint32_t)box, 32u, 1u}, elem[3] = {1u, 1u, 1u};
-    const CUresult r = ctx->encode_tiled(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, planes > 1 ? 3 : 2, base, dims,
-                                         strides, boxes, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                         box * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+    cuuint64_t dims[2] = {(cuuint64_t)columns, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(pitch * size)};
+    cuuint32_t box[2] = {(cuuint32_t)(64 / size), 32u}, elem[2] = {1u, 1u};
+    const CUresult r = ctx->encode_tiled(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, elem,
+                                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS)
-        return fail(ctx, TFJSB_ERR_CUDA, std::string("cuTensorMapEncodeTiled failed for ") + what + " (CUresult " + std::to_string((int)r) + ")");
+        return fail(ctx, TFJSB_ERR_CUDA, "cuTensorMapEncodeTiled failed for the result (CUresult " + std::to_string((int)r) + ")");
     return TFJSB_OK;
 }
 
@@ -928,20 +915,52 @@ double cost(const Product& p, const Shape& c, int sm_count) {
     };
     const double main = own_kb * k_block(c.subs), first = c.cg == 2 ? 4200 : 3400;
     const int columns = p.epilogue == EPI_GATED ? c.block_n / 2 : c.block_n;
-    const double chunk = p.epilogue == EPI_STORE ? 900. / 32 : p.epilogue == EPI_SCALE ? 1200. / 32 : p.epilogue == EPI_GRAD ? 1950. / 16 : a.z ? 1500. / 16 : 1000. / 16;
-    const double epilogue = columns / 2 * chunk * (p.planes == 3 ? 2.5 : 1);
+    const double chunk = p.epilogue == EPI_STORE ? 900. / 32 : p.epilogue == EPI_SCALE ? 1300. / 32 : p.epilogue == EPI_GRAD ? 1800. / 16 : a.z ? 1400. / 16 : 1200. / 16;
+    const double epilogue = columns / 4 * chunk * (p.planes == 3 ? 2.5 : 1);
     const int64_t tiles = tiles_of(p, c.cg, c.block_n, c.subs), slots = sm_count / c.cg;
     if (c.splits > 1) {
-        const int64_t shares = (int64_t)rows * (columns / 8), each = 256 * c.splits;
+        const int64_t shares = (int64_t)rows * (columns / 8), each = 32 * EPI_WARPS * c.splits;
         return first + main + 3200 + (double)((shares + each - 1) / each) * 2000;
     }
     const int64_t rounds = tiles / slots, rest = tiles % slots;
     if (c.subs == 2) {
-        const double whole = main + 0.8 * epilogue;
+        const double whole = main + 1.5 * epilogue;
         return first + rounds * whole + (rest == 0 ? 0. : 2 * rest <= slots ? own_kb * k_block(1) + epilogue : whole) + epilogue;
     }
     const double step = main > epilogue ? main : epilogue;
     return first + main + epilogue + (rounds + (rest ? 1 : 0) - 1) * step;
+}
+
+// Clusters of that many CTAs, one to an SM, that are resident at once: less than the SMs over their number, which the GPU's groups of SMs
+// do not divide.
+int resident_clusters(int size) {
+    static std::mutex mu;
+    static std::map<std::pair<int, int>, int> known;  // (device, size)
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+    std::lock_guard<std::mutex> lock(mu);
+    auto it = known.find({dev, size});
+    if (it != known.end()) return it->second;
+    auto* kernel = &dense_kernel<1, 1, KIND_BF16, EPI_STORE, 1, false, false>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(size * 64);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = tile::SMEM_LIMIT - 2048;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = size;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (smem_attr_once(reinterpret_cast<const void*>(kernel), tile::SMEM_LIMIT - 2048) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        n = 96 / size;
+    }
+    known[{dev, size}] = n;
+    return n;
 }
 
 Shape choose(const Product& p, int sm_count) {
@@ -959,7 +978,7 @@ Shape choose(const Product& p, int sm_count) {
             for (int splits = 1; splits <= (cg == 1 && bn <= 128 ? 8 : 1); splits *= 2) {
                 // at least four k-blocks a slice, none without any, one wave
                 const int each = (kb + splits - 1) / splits;
-                if (splits > 1 && (each < 4 || each * (splits - 1) >= kb || tiles * splits > sm_count)) continue;
+                if (splits > 1 && (each < 4 || each * (splits - 1) >= kb || tiles > resident_clusters(splits))) continue;
                 for (int subs = 1; subs <= (cg == 2 && bn == 256 && p.planes == 1 ? 2 : 1); ++subs) {
                     const Shape c = {cg, bn, splits, subs};
                     if (force && f[0] == cg && f[1] == bn && f[2] == splits && f[3] == subs) return c;
@@ -1001,7 +1020,7 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     a.dev_status = ctx->dev_status;
     const int own_n = c.block_n / c.cg;
     const int stage_bytes = p.planes * (c.subs * A_BYTES + own_n * 128);
-    const int slabs = 8 * (p.planes == 3 ? 0 : p.epilogue == EPI_GRAD ? SLAB_BYTES<1, EPI_GRAD> : SLAB_BYTES<1, EPI_STORE>);
+    const int slabs = EPI_WARPS * (p.planes == 1 && (p.epilogue == EPI_STORE || p.epilogue == EPI_SCALE) ? SLAB_BYTES<1, EPI_STORE> : 0);
     const int stages = (tile::SMEM_LIMIT - 2048 - 1024 - slabs) / stage_bytes;
     a.stages = stages < MAX_STAGES ? stages : MAX_STAGES;
     const size_t smem = 1024 + (size_t)a.stages * stage_bytes + slabs;
@@ -1013,11 +1032,10 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     maps.b[1] = maps.b[0];
     if (p.b[1].base && (st = encode(ctx, &maps.b[1], p.b[1], p.kind, a.N, a.K, b_rows, "B")) != TFJSB_OK) return st;
     if (p.planes == 1 && c.splits == 1) {
-        if (a.z && (st = encode_rows(ctx, &maps.z, a.z, true, a.N, a.M, 2, a.z_pitch, 16, "z")) != TFJSB_OK) return st;
         const bool f32 = p.epilogue == EPI_SCALE && !a.out_bf16;
         a.out_mapped = (p.epilogue == EPI_STORE || p.epilogue == EPI_SCALE) && a.out_pitch * (f32 ? 4 : 2) % 16 == 0;
         for (int i = 0; i < a.outputs && a.out_mapped; ++i)
-            if ((st = encode_rows(ctx, &maps.out[i], a.out[i], f32, a.N, a.M, 1, a.out_pitch, 32, "the result")) != TFJSB_OK) return st;
+            if ((st = encode_result(ctx, &maps.out[i], a.out[i], f32, a.N, a.M, a.out_pitch)) != TFJSB_OK) return st;
     }
     const int grid = (int)(c.splits > 1 ? tiles * c.splits : (tiles < slots ? tiles : slots) * c.cg);
     const cudaError_t e = c.subs == 2                      ? launch_any<2, 1, 2>(p, maps, grid, smem, s, &ctx->launches)

@@ -97,7 +97,7 @@ tfjsb_status sizes_of(const tfjsb_ffn* f, Sizes* s, std::string* why) {
     s->wd_bytes = up256(s->F * up8(s->Do) * e);
     s->dy_bytes = up256(s->T * up8(s->Do) * e);
     s->h_bytes = up256(s->T * s->fp * e);
-    s->z_bytes = up256(s->T * s->fp * 8);
+    s->z_bytes = up256((s->T + 31) / 32 * 32 * s->fp * 8);  // whole blocks of 32 rows
     s->grad_bytes = up256(s->T * s->fp * 2 * e);
     const int64_t weights = (s->repack_x ? s->x_bytes : 0) + (s->repack_up ? 2 * s->w_bytes : 0) + (s->repack_down ? s->wd_bytes : 0);
     s->few = s->T <= FEW_ROWS ? up256(s->T * s->F * 4) : 0;
