@@ -58,24 +58,23 @@ __device__ __forceinline__ uint64_t mn_desc(uint32_t addr) {
            (2ull << 61);
 }
 
+// Descriptors come as their lower words, which change from MMA to MMA, and their upper words, which do not: 32-bit additions on the
+// uniform datapath are most of what a k-block costs the issuing warp.
+#define TFJSB_DENSE_MMA(FORM)                                                                                                      \
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\tsetp.ne.b32 p, %6, 0;\n\t"     \
+                 "tcgen05.mma." FORM " [%0], a, b, %5, p;\n\t}" ::"r"(d), "r"(a), "r"(a_hi), "r"(b), "r"(b_hi), "r"(idesc), "r"(accumulate) \
+                 : "memory")
 template <int CG, int KIND>
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint32_t a_hi, uint32_t b, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
     if (KIND == KIND_BF16) {
-        if (CG == 2)
-            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-                         "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-        else
-            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-                         "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        if (CG == 2) TFJSB_DENSE_MMA("cta_group::2.kind::f16");
+        else TFJSB_DENSE_MMA("cta_group::1.kind::f16");
     } else {
-        if (CG == 2)
-            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-                         "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-        else
-            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-                         "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        if (CG == 2) TFJSB_DENSE_MMA("cta_group::2.kind::i8");
+        else TFJSB_DENSE_MMA("cta_group::1.kind::i8");
     }
 }
+#undef TFJSB_DENSE_MMA
 template <int CG>
 __device__ __forceinline__ void commit(uint32_t bar) {  // to this CTA, or to the same barrier of both
     if (CG == 2) tc_commit_pair(bar, (uint16_t)3);
@@ -102,7 +101,6 @@ __device__ __forceinline__ uint4 lds4_cluster(uint32_t addr) {
     return v;
 }
 
-__device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[32]) { tc_ld_32x32(at, r); }
 __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[16]) { tc_ld_cols(at, r); }
 __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[8]) { tc_ld_cols(at, r); }
 
@@ -332,6 +330,10 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
         constexpr int A_GROUPS = A_MN ? ROWS / 64 : 1, A_COPIES = SUBS * P * A_GROUPS;
         constexpr int B_MATS = EPI == EPI_GATED && CG == 1 ? 2 : 1, B_GROUPS = B_MN ? 4 / B_MATS / CG : 1, B_COPIES = P * B_MATS * B_GROUPS;
         const int mat_n = own_n / B_MATS, groups = B_MN ? mat_n / 64 : 1;
+        const uint32_t full_0 = smem_u32(&bar_full[0]), empty_0 = smem_u32(&bar_empty[0]), full_leader = CG == 2 ? map_to_cta(full_0, 0u) : full_0;
+        const uint32_t dst_0 = stage_base + (is_a ? 0u : SUBS * P * a_plane);
+        uint32_t dst = dst_0;
+        bool ready = false;  // the elected thread's: the stage was seen free while the one before was filled
         for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
             const Item it = item_at<SUBS>(args, tile);
             const int tn = it.tn;
@@ -339,12 +341,11 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
             const int m0 = it.tm * TILE_M + it.sub * (CG * ROWS) + (int)rank * ROWS;
             const int n0 = EPI == EPI_GATED ? tn * (block_n >> 1) : (tn - which * args.n_tiles) * block_n + (int)rank * own_n;
             const uint32_t tx = (uint32_t)it.subs * a_tx + b_tx;
+            int pass = kb_begin >= args.num_kb ? 1 : 0, k0 = (kb_begin - pass * args.num_kb) * BK;
             for (int kb = kb_begin; kb < kb_end; ++kb) {
-                const int pass = kb >= args.num_kb ? 1 : 0;
-                const int k0 = (kb - pass * args.num_kb) * BK;
-                const uint32_t own_full = smem_u32(&bar_full[stage]), empty = smem_u32(&bar_empty[stage]);
-                const uint32_t full = CG == 2 ? map_to_cta(own_full, 0u) : own_full;
-                const uint32_t dst = stage_base + (uint32_t)stage * stage_bytes + (is_a ? 0u : SUBS * P * a_plane);
+                const uint32_t own_full = full_0 + 8u * stage, empty = empty_0 + 8u * stage, full = full_leader + 8u * stage;
+                const int next = stage + 1 == stages ? 0 : stage + 1;
+                const uint32_t next_empty = empty_0 + 8u * next, next_phase = phase ^ (next == 0 ? 1u : 0u);
                 if (is_a) {
                     uint32_t to[A_COPIES];
                     int c0[A_COPIES], c1[A_COPIES], c2[A_COPIES];
@@ -352,12 +353,13 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                     for (int i = 0; i < A_COPIES; ++i) {
                         const int g = i % A_GROUPS, u = i / A_GROUPS % SUBS, p = i / A_GROUPS / SUBS;
                         const int row = m0 + u * (CG * ROWS) + 64 * g;
-                        to[i] = dst + (uint32_t)(p * SUBS + u) * a_plane + (uint32_t)g * GROUP_BYTES;
+                        to[i] = dst + (uint32_t)((p * SUBS + u) * A_BYTES + g * GROUP_BYTES);
                         c0[i] = A_MN ? row : k0;
                         c1[i] = A_MN ? k0 : row;
                         c2[i] = pass * P + p;
                     }
-                    if (elected && ok && (ok = bounded_wait(empty, phase ^ 1u, abort_flag))) {
+                    if (elected && ok && (ready || (ok = bounded_wait(empty, phase ^ 1u, abort_flag)))) {
+                        ready = mbar_test_wait(next_empty, next_phase ^ 1u);
                         if (leader) mbar_arrive_expect_tx(own_full, tx);
 #pragma unroll
                         for (int i = 0; i < A_COPIES; ++i)
@@ -378,14 +380,19 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                         c1[i] = B_MN ? k0 : row;
                         c2[i] = which * P + p;
                     }
-                    if (elected && ok && (ok = bounded_wait(empty, phase ^ 1u, abort_flag))) {
+                    if (elected && ok && (ready || (ok = bounded_wait(empty, phase ^ 1u, abort_flag)))) {
+                        ready = mbar_test_wait(next_empty, next_phase ^ 1u);
 #pragma unroll
                         for (int i = 0; i < B_COPIES; ++i)
                             if (i % B_GROUPS < groups) load3<CG>(to[i], B_MATS == 2 && i / B_GROUPS % B_MATS ? &map_b1 : map_b, full, c0[i], c1[i], c2[i]);
                         ++issued;
                     }
                 }
-                if (++stage == stages) { stage = 0; phase ^= 1u; }
+                stage = next;
+                phase = next_phase;
+                dst = next == 0 ? dst_0 : dst + stage_bytes;
+                k0 += BK;
+                if (kb + 1 == args.num_kb) { pass = 1; k0 = 0; }
             }
         }
         if (!ok) {
@@ -408,103 +415,117 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                                                        : (2u << 4) | (1u << 7) | (1u << 10);  // 32-bit sums of signed 8-bit
             const uint32_t idesc = formats | ((uint32_t)(block_n >> 3) << 17) | ((uint32_t)(CG * ROWS >> 4) << 24) |
                                    (A_MN ? IDESC_A_MN : 0u) | (B_MN ? IDESC_B_MN : 0u);
-            constexpr uint64_t a_step = A_MN ? 128 : 2, b_step = B_MN ? 128 : 2;  // of an MMA along K, in 16 bytes
+            constexpr uint32_t a_step = A_MN ? 128 : 2, b_step = B_MN ? 128 : 2;  // of an MMA along K, in 16 bytes
+            const uint64_t a_desc = A_MN ? mn_desc(stage_base) : make_kmajor_sw128_desc(stage_base);
+            const uint64_t b_desc = B_MN ? mn_desc(stage_base + SUBS * P * a_plane) : make_kmajor_sw128_desc(stage_base + SUBS * P * a_plane);
+            const uint32_t a_hi = (uint32_t)(a_desc >> 32), b_hi = (uint32_t)(b_desc >> 32), a_0 = (uint32_t)a_desc, b_0 = (uint32_t)b_desc;
+            const uint32_t stage_step = stage_bytes >> 4;
+            const uint32_t full_0 = smem_u32(&bar_full[0]), empty_0 = smem_u32(&bar_empty[0]), acc_full_0 = smem_u32(&bar_acc_full[0]), acc_empty_0 = smem_u32(&bar_acc_empty[0]);
             int stage = 0;
             uint32_t phase = 0;
-            int acc = 0;
-            uint32_t acc_phase = 0;
+            uint32_t offset = 0;  // of the stage, in 16 bytes
             const bool elected = elect_one();
-            bool ok = true;  // the elected thread's
-            bool issued_any = false;
+            bool ok = true, issued_any = false, ready = false;  // the elected thread's; ready: the stage was seen filled
+            auto advance = [&]() {
+                const bool wrap = stage + 1 == stages;
+                stage = wrap ? 0 : stage + 1;
+                phase ^= wrap ? 1u : 0u;
+                offset = wrap ? 0u : offset + stage_step;
+            };
             if constexpr (SUBS == 2) {
                 // Both parts of a tile use each stage.  At its beginning and its end a part's MMAs of LEAD k-blocks go one after
                 // the other: the first part is complete, and read by the epilogue, while the second is still summed, and the
                 // next tile begins in the first part's columns while the second part's are read.
                 constexpr int LEAD = 2;
                 uint32_t part_phase[2] = {0u, 0u};
-                auto issue = [&](int at_stage, uint32_t at_phase, int part, bool first, bool wait) {
-                    const uint32_t base = stage_base + (uint32_t)at_stage * stage_bytes, a_addr = base + (uint32_t)part * a_plane;
-                    const uint32_t b_addr = base + 2 * a_plane;
-                    uint64_t da[4], db[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        da[k] = (A_MN ? mn_desc(a_addr) : make_kmajor_sw128_desc(a_addr)) + a_step * k;
-                        db[k] = (B_MN ? mn_desc(b_addr) : make_kmajor_sw128_desc(b_addr)) + b_step * k;
-                    }
-                    const uint32_t d = tmem_base + (uint32_t)part * acc_cols, full = smem_u32(&bar_full[at_stage]), begun = first ? 0u : 1u;
-                    if (elected && ok && (!wait || (ok = bounded_wait(full, at_phase, abort_flag)))) {
-                        if (wait) tc_fence_after();
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) mma<CG, KIND>(d, da[k], db[k], idesc, k == 0 ? begun : 1u);
-                        issued_any = true;
-                    }
-                };
                 for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
                     const int subs = item_at<SUBS>(args, tile).subs;
                     for (int kb = kb_begin; kb < kb_end;) {
                         // k-blocks of one part in a row
                         const int run = kb == kb_begin || kb_end - kb <= LEAD ? min(LEAD, kb_end - kb) : 1;
-                        int st = stage;
-                        uint32_t ph = phase;
-                        for (int part = 0; part < subs; ++part) {
+                        const int stage_was = stage;
+                        const uint32_t phase_was = phase, offset_was = offset;
+#pragma unroll
+                        for (int part = 0; part < 2; ++part) {
+                            if (part >= subs) break;
                             if (kb == kb_begin) {
-                                if (elected && ok) ok = bounded_wait(smem_u32(&bar_acc_empty[part]), part_phase[part] ^ 1u, abort_flag);
+                                if (elected && ok) ok = bounded_wait(acc_empty_0 + 8u * part, part_phase[part] ^ 1u, abort_flag);
                                 part_phase[part] ^= 1u;
                                 tc_fence_after();
                             }
-                            st = stage;
-                            ph = phase;
+                            stage = stage_was;
+                            phase = phase_was;
+                            offset = offset_was;
+                            const uint32_t d = tmem_base + (uint32_t)part * acc_cols;
                             for (int j = 0; j < run; ++j) {
-                                issue(st, ph, part, kb + j == kb_begin, part == 0);
-                                if (part + 1 == subs && elected && ok) commit<CG>(smem_u32(&bar_empty[st]));
-                                if (++st == stages) { st = 0; ph ^= 1u; }
+                                const uint32_t a0 = a_0 + offset + (uint32_t)(part * (A_BYTES >> 4)), b0 = b_0 + offset, full = full_0 + 8u * stage, empty = empty_0 + 8u * stage;
+                                const uint32_t a1 = a0 + a_step, a2 = a0 + 2 * a_step, a3 = a0 + 3 * a_step, b1 = b0 + b_step, b2 = b0 + 2 * b_step, b3 = b0 + 3 * b_step;
+                                const uint32_t begun = kb + j == kb_begin ? 0u : 1u;
+                                const bool last = part + 1 == subs;
+                                advance();
+                                const uint32_t next_full = full_0 + 8u * stage, next_phase = phase, this_phase = phase ^ (stage == 0 ? 1u : 0u);
+                                if (elected && ok && (part > 0 || ready || (ok = bounded_wait(full, this_phase, abort_flag)))) {
+                                    if (part == 0) tc_fence_after();
+                                    ready = mbar_test_wait(next_full, next_phase);
+                                    mma<CG, KIND>(d, a0, a_hi, b0, b_hi, idesc, begun);
+                                    mma<CG, KIND>(d, a1, a_hi, b1, b_hi, idesc, 1u);
+                                    mma<CG, KIND>(d, a2, a_hi, b2, b_hi, idesc, 1u);
+                                    mma<CG, KIND>(d, a3, a_hi, b3, b_hi, idesc, 1u);
+                                    if (last) commit<CG>(empty);
+                                    issued_any = true;
+                                }
                             }
-                            if (kb + run == kb_end && elected && ok) commit<CG>(smem_u32(&bar_acc_full[part]));
+                            if (kb + run == kb_end && elected && ok) commit<CG>(acc_full_0 + 8u * part);
                         }
-                        stage = st;
-                        phase = ph;
                         kb += run;
                     }
                 }
-            } else for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
-                int in_segment = 0;
-                for (int kb = kb_begin; kb < kb_end; ++kb) {
-                    if (in_segment == 0 && elected && ok) ok = bounded_wait(smem_u32(&bar_acc_empty[acc]), acc_phase ^ 1u, abort_flag);
-                    const uint32_t d = tmem_base + (uint32_t)acc * acc_cols;
-                    const uint32_t a_addr = stage_base + (uint32_t)stage * stage_bytes, b_addr = a_addr + P * a_plane;
-                    uint64_t da[P][4], db[P][4];
-#pragma unroll
-                    for (int p = 0; p < P; ++p)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            da[p][k] = (A_MN ? mn_desc(a_addr + p * a_plane) : make_kmajor_sw128_desc(a_addr + p * a_plane)) + a_step * k;
-                            db[p][k] = (B_MN ? mn_desc(b_addr + p * b_plane) : make_kmajor_sw128_desc(b_addr + p * b_plane)) + b_step * k;
+            } else {
+                int acc = 0;
+                uint32_t acc_phase = 0;
+                for (int tile = first_tile; tile < args.num_tiles; tile += tile_step) {
+                    int in_segment = 0;
+                    for (int kb = kb_begin; kb < kb_end; ++kb) {
+                        if (in_segment == 0 && elected && ok) {
+                            ok = bounded_wait(acc_empty_0 + 8u * acc, acc_phase ^ 1u, abort_flag);
+                            tc_fence_after();
                         }
-                    const uint32_t begun = in_segment != 0 ? 1u : 0u, full = smem_u32(&bar_full[stage]), empty = smem_u32(&bar_empty[stage]);
-                    const uint32_t small = d + (uint32_t)block_n;
-                    if (elected && ok && (ok = bounded_wait(full, phase, abort_flag))) {
-                        tc_fence_after();
+                        const uint32_t d = tmem_base + (uint32_t)acc * acc_cols, small = d + (uint32_t)block_n;
+                        uint32_t a[P][4], b[P][4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t more = k == 0 ? begun : 1u;
-                            mma<CG, KIND>(d, da[0][k], db[0][k], idesc, more);
-                            if constexpr (P == 3) {
-                                mma<CG, KIND>(small, da[2][k], db[0][k], idesc, more);
-                                mma<CG, KIND>(small, da[0][k], db[2][k], idesc, 1u);
-                                mma<CG, KIND>(small, da[1][k], db[1][k], idesc, 1u);
-                                mma<CG, KIND>(small, da[1][k], db[0][k], idesc, 1u);
-                                mma<CG, KIND>(small, da[0][k], db[1][k], idesc, 1u);
+                        for (int p = 0; p < P; ++p)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                a[p][k] = a_0 + offset + (uint32_t)(p * (A_BYTES >> 4)) + a_step * k;
+                                b[p][k] = b_0 + offset + (uint32_t)p * (b_plane >> 4) + b_step * k;
                             }
+                        const uint32_t begun = in_segment != 0 ? 1u : 0u, full = full_0 + 8u * stage, empty = empty_0 + 8u * stage;
+                        advance();
+                        const uint32_t next_full = full_0 + 8u * stage, next_phase = phase, this_phase = phase ^ (stage == 0 ? 1u : 0u);
+                        if (elected && ok && (ready || (ok = bounded_wait(full, this_phase, abort_flag)))) {
+                            tc_fence_after();
+                            ready = mbar_test_wait(next_full, next_phase);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const uint32_t more = k == 0 ? begun : 1u;
+                                mma<CG, KIND>(d, a[0][k], a_hi, b[0][k], b_hi, idesc, more);
+                                if constexpr (P == 3) {
+                                    mma<CG, KIND>(small, a[2][k], a_hi, b[0][k], b_hi, idesc, more);
+                                    mma<CG, KIND>(small, a[0][k], a_hi, b[2][k], b_hi, idesc, 1u);
+                                    mma<CG, KIND>(small, a[1][k], a_hi, b[1][k], b_hi, idesc, 1u);
+                                    mma<CG, KIND>(small, a[1][k], a_hi, b[0][k], b_hi, idesc, 1u);
+                                    mma<CG, KIND>(small, a[0][k], a_hi, b[1][k], b_hi, idesc, 1u);
+                                }
+                            }
+                            commit<CG>(empty);
+                            issued_any = true;
                         }
-                        commit<CG>(empty);
-                        issued_any = true;
-                    }
-                    if (++stage == stages) { stage = 0; phase ^= 1u; }
-                    ++in_segment;
-                    if (kb + 1 == kb_end || (P == 3 && in_segment == args.seg_kb)) {
-                        if (elected && ok) commit<CG>(smem_u32(&bar_acc_full[acc]));
-                        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
-                        in_segment = 0;
+                        ++in_segment;
+                        if (kb + 1 == kb_end || (P == 3 && in_segment == args.seg_kb)) {
+                            if (elected && ok) commit<CG>(acc_full_0 + 8u * acc);
+                            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+                            in_segment = 0;
+                        }
                     }
                 }
             }
