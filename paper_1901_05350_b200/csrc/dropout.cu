@@ -20,7 +20,7 @@ namespace tfjsb {
 namespace {
 
 constexpr int PER_THREAD = 8, BLOCK = 256;
-constexpr uint32_t MULTIPLIER[2] = {0xD2511F53u, 0xCD9E8D57u}, KEY_STEP[2] = {0x9E3779B9u, 0xBB67AE85u};
+constexpr uint32_t MULTIPLIER_0 = 0xD2511F53u, MULTIPLIER_1 = 0xCD9E8D57u, KEY_STEP[2] = {0x9E3779B9u, 0xBB67AE85u};
 constexpr int ROUNDS = 10;
 
 struct DropoutArgs {
@@ -39,29 +39,38 @@ struct DropoutArgs {
     uint64_t extent[4], step[4];
 };
 
+__device__ __forceinline__ void multiply(uint32_t a, uint32_t m, uint32_t& high, uint32_t& low) {
+    uint64_t p;
+    asm("mul.wide.u32 %0, %1, %2;" : "=l"(p) : "r"(a), "r"(m));
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(low), "=r"(high) : "l"(p));
+}
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0x96;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+
 // The four words of a block.  The offset is the same for all, so one product of the first round is worked out before the launch, and so is one of
 // the second where the upper half of the block's index is 0 (SMALL: less than 2^34 elements).  The multiplier that makes 64 bits of 32 is
 // what bounds the kernel next to memory: 18 of them a block instead of 20.
 template <bool SMALL>
 __device__ __forceinline__ void philox(const DropoutArgs& a, uint64_t block, uint32_t (&w)[4]) {
-    const uint64_t first = (uint64_t)(uint32_t)block * MULTIPLIER[0];
-    uint32_t c0 = a.high1, c1 = a.low1, c2 = (uint32_t)(first >> 32) ^ a.offset[1] ^ a.keys[0][1], c3 = (uint32_t)first;
+    uint32_t h0, l0, h1, l1;
+    multiply((uint32_t)block, MULTIPLIER_0, h0, l0);
+    uint32_t c0 = a.high1, c1 = a.low1, c2 = xor3(h0, a.offset[1], a.keys[0][1]), c3 = l0;
     if (!SMALL) c0 ^= (uint32_t)(block >> 32);
 #pragma unroll
     for (int r = 1; r < ROUNDS; ++r) {
-        const uint64_t p1 = (uint64_t)c2 * MULTIPLIER[1];
-        uint32_t h0, l0;
+        multiply(c2, MULTIPLIER_1, h1, l1);
         if (SMALL && r == 1) {
             h0 = a.high2;
             l0 = a.low2;
         } else {
-            const uint64_t p0 = (uint64_t)c0 * MULTIPLIER[0];
-            h0 = (uint32_t)(p0 >> 32);
-            l0 = (uint32_t)p0;
+            multiply(c0, MULTIPLIER_0, h0, l0);
         }
-        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ a.keys[r][0];
-        c2 = h0 ^ c3 ^ a.keys[r][1];
-        c1 = (uint32_t)p1;
+        c0 = xor3(h1, c1, a.keys[r][0]);
+        c2 = xor3(h0, c3, a.keys[r][1]);
+        c1 = l1;
         c3 = l0;
     }
     w[0] = c0; w[1] = c1; w[2] = c2; w[3] = c3;
@@ -165,11 +174,15 @@ __device__ __forceinline__ void load8(const void* p, int64_t i, int left, float 
     }
 }
 
+// A block has STEPS pieces of 2048 elements: many more blocks than are resident, so that those on SMs with less to wait for take more of
+// them (one wave of blocks that each did the same share left the SMs at 70 % of their warps, 73 us for 67 M bfloat16 values against 67).
+constexpr int STEPS = 4;
 template <bool F32, bool BROADCAST, bool RESIDUAL, typename I>
 __global__ void __launch_bounds__(BLOCK) dropout_kernel(const __grid_constant__ DropoutArgs a) {
     ptx::pdl_wait();
-    const int64_t step = (int64_t)gridDim.x * BLOCK * PER_THREAD;
-    for (int64_t i = ((int64_t)blockIdx.x * BLOCK + threadIdx.x) * PER_THREAD; i < a.n; i += step) {
+    int64_t i = (int64_t)blockIdx.x * (STEPS * BLOCK * PER_THREAD) + threadIdx.x * PER_THREAD;
+#pragma unroll 1
+    for (int step = 0; step < STEPS && i < a.n; ++step, i += BLOCK * PER_THREAD) {
         const int left = a.n - i < 8 ? (int)(a.n - i) : 8;
         float x[8], r[8];
         load8<F32>(a.x, i, left, x);
@@ -186,22 +199,118 @@ __global__ void __launch_bounds__(BLOCK) dropout_kernel(const __grid_constant__ 
     }
 }
 
+// A mask shared by many positions: [outer][positions][channels], one row of the mask for all positions of an outer index (spatial dropout of
+// a sequence or an image).  A thread has four channels, whose words it makes once, of `share` positions: next to no arithmetic is left, so
+// this is bound by memory where making each word again was bound by the generator (64 x 197 x 771 fp32: 28 us).  VECTOR: rows of
+// channels are whole groups of four.
+struct Positions {
+    int64_t outer, positions, groups;  // groups of four channels
+    int share;
+};
+template <bool F32, bool RESIDUAL, bool VECTOR>
+__global__ void __launch_bounds__(BLOCK) dropout_positions_kernel(const __grid_constant__ DropoutArgs a, const __grid_constant__ Positions s) {
+    ptx::pdl_wait();
+    const int64_t t = (int64_t)blockIdx.x * BLOCK + threadIdx.x, o = t / s.groups;
+    if (o >= s.outer) return;
+    const int64_t channels = (int64_t)a.extent[0], c = (t - o * s.groups) * 4;
+    const int left = channels - c < 4 ? (int)(channels - c) : 4;
+    uint64_t m = (uint64_t)c, rest = (uint64_t)o;
+    for (int d = 2; d < a.dims; ++d) {
+        const uint64_t q = rest / a.extent[d];
+        m += (rest - q * a.extent[d]) * a.step[d];
+        rest = q;
+    }
+    uint32_t w[8];
+    run_of_words<false>(a, m, w);
+    bool keep[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) keep[e] = w[e] >= a.threshold;
+    const int64_t first = (int64_t)blockIdx.y * s.share, last = first + s.share < s.positions ? first + s.share : s.positions;
+    auto load4 = [&](const void* p, int64_t i, float (&v)[4]) {
+        if (F32) {
+            const float* q = static_cast<const float*>(p) + i;
+            if (VECTOR) {
+                const float4 f = ld_global4(q);
+                v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = e < left ? load_global(q + e) : 0.f;
+            }
+        } else {
+            const unsigned short* q = static_cast<const unsigned short*>(p) + i;
+            if (VECTOR) {
+                const uint2 f = load_global(reinterpret_cast<const uint2*>(q));
+                v[0] = __uint_as_float(f.x << 16); v[1] = __uint_as_float(f.x & 0xffff0000u);
+                v[2] = __uint_as_float(f.y << 16); v[3] = __uint_as_float(f.y & 0xffff0000u);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = e < left ? __uint_as_float((uint32_t)load_global(q + e) << 16) : 0.f;
+            }
+        }
+    };
+    constexpr int U = 4;  // positions on their way at a time
+    for (int64_t p = first; p < last; p += U) {
+        float x[U][4], r[U][4];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u < last) {
+                const int64_t i = (o * s.positions + p + u) * channels + c;
+                load4(a.x, i, x[u]);
+                if (RESIDUAL) load4(a.residual, i, r[u]);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u < last) {
+                const int64_t i = (o * s.positions + p + u) * channels + c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (RESIDUAL) x[u][e] = keep[e] ? fmaf(x[u][e], a.scale, r[u][e]) : r[u][e];
+                    else x[u][e] = keep[e] ? x[u][e] * a.scale : 0.f;
+                }
+                if (F32) {
+                    float* q = static_cast<float*>(a.out) + i;
+                    if (VECTOR) *reinterpret_cast<float4*>(q) = make_float4(x[u][0], x[u][1], x[u][2], x[u][3]);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (e < left) q[e] = x[u][e];
+                } else {
+                    __nv_bfloat16* q = static_cast<__nv_bfloat16*>(a.out) + i;
+                    if (VECTOR) *reinterpret_cast<uint2*>(q) = make_uint2(dense::pack_bf16(x[u][0], x[u][1]), dense::pack_bf16(x[u][2], x[u][3]));
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (e < left) q[e] = __float2bfloat16_rn(x[u][e]);
+                }
+            }
+    }
+}
+
 template <bool F32, bool BROADCAST, bool RESIDUAL, typename I>
-cudaError_t launch(const DropoutArgs& a, int sm_count, cudaStream_t s) {
-    auto* kernel = &dropout_kernel<F32, BROADCAST, RESIDUAL, I>;
-    // One wave of blocks, so that none is left over for a second.
-    static const int resident = [kernel] {
-        int n = 0;
-        return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, BLOCK, 0) == cudaSuccess && n > 0 ? n : 1;
-    }();
-    const int64_t needed = (a.n + BLOCK * PER_THREAD - 1) / (BLOCK * PER_THREAD), most = (int64_t)sm_count * resident;
-    return launch_k(kernel, dim3((unsigned)(needed < most ? needed : most)), dim3(BLOCK), 0, s, a);
+cudaError_t launch(const DropoutArgs& a, cudaStream_t s) {
+    const int64_t blocks = (a.n + STEPS * BLOCK * PER_THREAD - 1) / (STEPS * BLOCK * PER_THREAD);
+    return launch_k(&dropout_kernel<F32, BROADCAST, RESIDUAL, I>, dim3((unsigned)blocks), dim3(BLOCK), 0, s, a);
 }
 template <bool F32, bool RESIDUAL>
 cudaError_t launch_any(const DropoutArgs& a, int sm_count, cudaStream_t s) {
+    // One row of the mask for at least eight positions, and enough threads with four channels of eight or more positions to fill the GPU
+    if (a.dims >= 2 && a.step[0] == 1 && a.step[1] == 0 && a.extent[1] >= 8) {
+        Positions p;
+        p.positions = (int64_t)a.extent[1];
+        p.groups = ((int64_t)a.extent[0] + 3) / 4;
+        p.outer = a.n / (int64_t)(a.extent[0] * a.extent[1]);
+        const int64_t threads = p.outer * p.groups, blocks = (threads + BLOCK - 1) / BLOCK;
+        p.share = 32;
+        while (p.share > 8 && blocks * ((p.positions + p.share - 1) / p.share) < (int64_t)sm_count * 8) p.share /= 2;
+        const int64_t shares = (p.positions + p.share - 1) / p.share;
+        if (a.extent[0] >= 32 && blocks < (1LL << 31) && shares <= 65535) {
+            auto* kernel = a.extent[0] % 4 == 0 ? &dropout_positions_kernel<F32, RESIDUAL, true> : &dropout_positions_kernel<F32, RESIDUAL, false>;
+            return launch_k(kernel, dim3((unsigned)blocks, (unsigned)shares), dim3(BLOCK), 0, s, a, p);
+        }
+    }
     const bool small = a.n < (1LL << 31);
-    if (a.dims == 0) return small ? launch<F32, false, RESIDUAL, uint32_t>(a, sm_count, s) : launch<F32, false, RESIDUAL, uint64_t>(a, sm_count, s);
-    return small ? launch<F32, true, RESIDUAL, uint32_t>(a, sm_count, s) : launch<F32, true, RESIDUAL, uint64_t>(a, sm_count, s);
+    if (a.dims == 0) return small ? launch<F32, false, RESIDUAL, uint32_t>(a, s) : launch<F32, false, RESIDUAL, uint64_t>(a, s);
+    return small ? launch<F32, true, RESIDUAL, uint32_t>(a, s) : launch<F32, true, RESIDUAL, uint64_t>(a, s);
 }
 
 bool overlaps_partly(const void* a, const void* b, int64_t bytes) {
@@ -228,7 +337,7 @@ tfjsb_status run(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, const char* x
     }
     if (empty) return TFJSB_OK;
     for (int d = 0; d < rank; ++d) {
-        if (dims[d] > (1LL << 42) / a.n) return fail(ctx, TFJSB_ERR_SHAPE, "more than 2^42 elements");
+        if (dims[d] > (1LL << 40) / a.n) return fail(ctx, TFJSB_ERR_SHAPE, "more than 2^40 elements");
         a.n *= dims[d];
     }
     if (!x || !out) return fail(ctx, TFJSB_ERR_INVALID_ARG, std::string(x_name) + " / " + out_name + " is null");
@@ -247,10 +356,10 @@ tfjsb_status run(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, const char* x
         for (int k = 0; k < 2; ++k) a.keys[r][k] = (uint32_t)(seed >> (32 * k)) + (uint32_t)r * KEY_STEP[k];
     a.offset[0] = (uint32_t)offset;
     a.offset[1] = (uint32_t)(offset >> 32);
-    const uint64_t p1 = (uint64_t)a.offset[0] * MULTIPLIER[1];
+    const uint64_t p1 = (uint64_t)a.offset[0] * MULTIPLIER_1;
     a.high1 = (uint32_t)(p1 >> 32) ^ a.keys[0][0];
     a.low1 = (uint32_t)p1;
-    const uint64_t p2 = (uint64_t)a.high1 * MULTIPLIER[0];
+    const uint64_t p2 = (uint64_t)a.high1 * MULTIPLIER_0;
     a.high2 = (uint32_t)(p2 >> 32);
     a.low2 = (uint32_t)p2;
     if (noise) {

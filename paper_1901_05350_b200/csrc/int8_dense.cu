@@ -65,9 +65,75 @@ __global__ void __launch_bounds__(QUANTIZE_THREADS) quantize_kernel(const void* 
     }
 }
 
+// A warp has a row, which it holds as it is stored: many rows whose length is a multiple of eight, up to GROUPS * 256 bfloat16 or GROUPS * 128
+// fp32 values.  No block waits for its slowest load, and an SM has 160 KiB of rows on their way (8192 x 4096 bfloat16: a block a row 32 us).
+template <bool F32, int GROUPS>
+__global__ void __launch_bounds__(128) quantize_rows_kernel(const void* x, int64_t rows, int64_t columns, int64_t pitch, int8_t* q, float* scale) {
+    ptx::pdl_wait();
+    ptx::pdl_launch_dependents();
+    constexpr int PER = F32 ? 4 : 8;  // values of 16 bytes
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (row >= rows) return;
+    const uint4* in = reinterpret_cast<const uint4*>(static_cast<const char*>(x) + row * columns * (F32 ? 4 : 2));
+    const int pieces = (int)(columns / PER);
+    uint4 v[GROUPS];
+#pragma unroll
+    for (int j = 0; j < GROUPS; ++j) {
+        v[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (j * 32 + lane < pieces)
+            asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[j].x), "=r"(v[j].y), "=r"(v[j].z), "=r"(v[j].w) : "l"(in + j * 32 + lane));
+    }
+    float amax;
+    if (F32) {
+        amax = 0.f;
+#pragma unroll
+        for (int j = 0; j < GROUPS; ++j) {
+            amax = max_nan(amax, max_nan(fabsf(__uint_as_float(v[j].x)), fabsf(__uint_as_float(v[j].y))));
+            amax = max_nan(amax, max_nan(fabsf(__uint_as_float(v[j].z)), fabsf(__uint_as_float(v[j].w))));
+        }
+    } else {
+        uint32_t m = 0u;  // two bfloat16
+        auto more = [&](uint32_t w) { asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w & 0x7fff7fffu)); };
+#pragma unroll
+        for (int j = 0; j < GROUPS; ++j) { more(v[j].x); more(v[j].y); more(v[j].z); more(v[j].w); }
+        amax = max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    const RowScale r = row_scale(amax);
+    if (lane == 0) scale[row] = amax / 127.f;
+    int8_t* out = q + row * pitch;
+#pragma unroll
+    for (int j = 0; j < GROUPS; ++j) {
+        const int at = j * 32 + lane;
+        if (at >= pieces) continue;
+        const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+        float f[8];
+        if (F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { f[e] = __uint_as_float(w[e]); f[e + 4] = 0.f; }
+            *reinterpret_cast<uint32_t*>(out + at * 4) = quantize8<true>(f, r).x;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(w[e] << 16); f[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
+            *reinterpret_cast<uint2*>(out + at * 8) = quantize8<false>(f, r);
+        }
+    }
+    if (columns + lane * 4 < pitch) *reinterpret_cast<uint32_t*>(out + columns + lane * 4) = 0u;  // a filled-up end of 4 or 8
+}
+
 template <bool F32>
 cudaError_t launch_quantize_as(const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, cudaStream_t s) {
     const int64_t pitch = (columns + 15) / 16 * 16;
+    // a warp a row where that is enough warps for the GPU
+    if (rows >= 148 * 8 && columns % 8 == 0 && columns <= (F32 ? 2048 : 4096)) {
+        constexpr int ALL = 16;
+        auto* kernel = columns <= (F32 ? 512 : 1024) ? &quantize_rows_kernel<F32, ALL / 4>
+                       : columns <= (F32 ? 1024 : 2048) ? &quantize_rows_kernel<F32, ALL / 2>
+                                                        : &quantize_rows_kernel<F32, ALL>;
+        return launch_k(kernel, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, s, x, rows, columns, pitch, q, scale);
+    }
     auto* kernel = columns <= 2048 ? &quantize_kernel<F32, 1> : columns <= 4096 ? &quantize_kernel<F32, 2> : &quantize_kernel<F32, 4>;
     return launch_k(kernel, dim3((unsigned)rows), dim3(QUANTIZE_THREADS), 0, s, x, columns, pitch, q, scale);
 }

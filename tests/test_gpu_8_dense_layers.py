@@ -88,6 +88,7 @@ def test_ffn_gates(ctx, gate, dtype):
     ((1,), None), ((7,), None), ((8,), None), ((1000,), None), ((4097,), None), ((128, 1000), None), ((3, 5, 7), (3, 1, 7)), ((3, 5, 7), (1, 5, 1)),
     ((4, 33, 64), (4, 1, 64)), ((4, 33, 65), (4, 1, 65)), ((16, 300), (16, 1)), ((16, 300), (1, 300)), ((2, 3, 4, 5), (2, 1, 4, 1)),
     ((2, 1, 40, 9), (1, 1, 40, 9)), ((9, 8), (1, 1)), ((6, 11), (6, 11)), ((2, 70, 3, 50), (2, 70, 1, 50)), ((700, 3), (1, 3)),
+    ((5, 3, 20, 37), (5, 3, 1, 37)), ((3, 40, 33), (1, 1, 33)), ((3, 4, 16, 50), (1, 4, 1, 50)), ((2, 100, 64), (2, 1, 64)), ((9, 197, 771), (9, 1, 771)),
 ], ids=str)
 def test_dropout(ctx, shape, noise, dtype):
     x, r = normal(1, shape, 1.0, dtype), normal(2, shape, 1.0, dtype)
@@ -106,7 +107,8 @@ def test_dropout(ctx, shape, noise, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=ids)
-@pytest.mark.parametrize("rows,columns", [(1, 1), (1, 16), (3, 17), (5, 100), (128, 1024), (7, 2047), (4, 8192), (3, 9001), (2, 20000)])
+@pytest.mark.parametrize("rows,columns", [(1, 1), (1, 16), (3, 17), (5, 100), (128, 1024), (7, 2047), (4, 8192), (3, 9001), (2, 20000),
+                                          (1500, 8), (1200, 24), (1300, 264), (1201, 1000), (1184, 2048), (1190, 2056), (1190, 4096), (1190, 4088), (1190, 5000), (1300, 33)])
 def test_quantized_rows(ctx, rows, columns, dtype):
     x = normal(rows + columns, (rows, columns), 1.0, dtype)
     x[0, 0] = 4.0  # halves of the largest value lie on the middle between two integers
