@@ -42,6 +42,9 @@ struct Args {
     int gate = 0;
     int out_bf16 = 1, act = 0;             // EPI_SCALE
     const float *a_scale = nullptr, *b_scale = nullptr, *bias = nullptr;
+    // The kernel before in the stream, one of this chain, writes nothing of the operand (nor may it still be running with what it
+    // waited for unfinished: kernels of a chain let the next one go after their own wait).
+    int early_a = 0, early_b = 0;
     unsigned int* dev_status = nullptr;
 };
 

@@ -314,14 +314,17 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
     }
     tc_fence_after();
     const uint32_t tmem_base = tmem_base_slot;
-    pdl_launch_dependents();
-    pdl_wait();
+    // Each role waits for the kernel before on its own: the producers only where that kernel may still write what they read (args.early_*), the
+    // epilogue always, before it reads or writes anything, and the next kernel is let go after that wait.  So when a kernel of a chain
+    // starts, everything but the kernel right before it is complete: it may read what the one before that wrote, and as SMs run out of tiles
+    // of one product they sum those of the next.
 
     if (warp == 0 || warp == B_WARP) {
         // ---------------------------------------------------------------- producers: of A (which arms the barriers) and of B
         // One thread issues a copy in 150 to 250 cycles, so the two operands have a warp each, and everything that an issue takes is
         // worked out by the whole warp outside the branch (see elect_one).
         const bool is_a = warp == 0;
+        if (!(is_a ? args.early_a : args.early_b)) pdl_wait();
         int stage = 0;
         uint32_t phase = 0;
         int issued = 0;
@@ -546,6 +549,8 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
         // 150, its buffer being read 230, the gate 400), so there are many warps.  The loop over chunks is rolled: a
         // short call runs its code once, and fetching it unrolled takes longer than the work.
         constexpr int PARTS = EPI_WARPS / 4;
+        pdl_wait();
+        pdl_launch_dependents();
         const int quad = warp & 3, part = (warp - 2) >> 2;
         const bool elected = elect_one();  // issues the warp's copies
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;

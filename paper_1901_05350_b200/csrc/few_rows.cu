@@ -28,10 +28,8 @@ constexpr int COLUMNS = 64;   // of a block: 8 groups of 8
 constexpr int K_LANES = 32;   // threads of a column group
 constexpr int CHUNK = 2048;   // values of a row of x in shared memory at a time
 
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
+__device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 __device__ __forceinline__ uint4 ld_weights(const void* p) {  // read once: not kept in L1
     uint4 v;
@@ -88,7 +86,7 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant
     constexpr int U = T >= 8 ? 4 : 8;  // rows of weights in flight a thread and matrix
     extern __shared__ float xs[];      // [k][T] of this slice, a chunk at a time
     __shared__ float part[WARPS][M][T * 8][8];
-    __shared__ float sums[M][T][COLUMNS];
+    __shared__ float sums[M][T][COLUMNS];  // [slice][column of this CTA's share]: every CTA of the cluster writes its slice's part
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = lane & 7, k_lane = warp * 4 + (lane >> 3);
     const uint32_t slice = a.splits > 1 ? cluster_ctarank() : 0u;
@@ -96,12 +94,26 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant
     const int left = (int)min((int64_t)8, a.N - c);
     const int k_begin = (int)slice * a.k_per_slice, k_end = min(a.K, k_begin + a.k_per_slice);
     float acc[M][T][8] = {};
+    if (a.splits > 1) cluster_arrive();  // "has begun", which the others wait for before they write here
+    Eight<F32> w[M][U];
+    auto fetch = [&](int k0, int count, int k) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (k + u * K_LANES < count && left > 0) {
+                w[0][u].template load<VECTOR>(a.w0, k0 + k + u * K_LANES, a.N, c, left);
+                if (GATED) w[M - 1][u].template load<VECTOR>(a.w1, k0 + k + u * K_LANES, a.N, c, left);
+            }
+    };
+    // The second kernel of a block follows the first, which writes no weights and lets this one start once everything before it is
+    // done: its first weights are on their way while the first kernel runs.
+    if (!GATED) fetch(k_begin, min(CHUNK, k_end - k_begin), k_lane);
     pdl_wait();
     pdl_launch_dependents();
 
     for (int k0 = k_begin; k0 < k_end; k0 += CHUNK) {
         const int count = min(CHUNK, k_end - k0);
         if (k0 != k_begin) __syncthreads();
+        if (GATED || k0 != k_begin) fetch(k0, count, k_lane);  // on its way while x is
         for (int i = threadIdx.x; i < count * T; i += THREADS) {
             const int t = i / count, k = i - t * count;  // rows of x along threads
             float v = 0.f;
@@ -112,16 +124,6 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant
             }
             xs[k * T + t] = v;
         }
-        Eight<F32> w[M][U];
-        auto fetch = [&](int k) {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (k + u * K_LANES < count && left > 0) {
-                    w[0][u].template load<VECTOR>(a.w0, k0 + k + u * K_LANES, a.N, c, left);
-                    if (GATED) w[M - 1][u].template load<VECTOR>(a.w1, k0 + k + u * K_LANES, a.N, c, left);
-                }
-        };
-        fetch(k_lane);  // on its way while x is
         __syncthreads();
         for (int k = k_lane; k < count; k += U * K_LANES) {
 #pragma unroll
@@ -139,7 +141,7 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant
                             for (int t = 0; t < T; ++t) acc[m][t][i] = fmaf(x[t], v, acc[m][t][i]);
                         }
                 }
-            if (k + U * K_LANES < count) fetch(k + U * K_LANES);
+            if (k + U * K_LANES < count) fetch(k0, count, k + U * K_LANES);
         }
     }
 
@@ -162,30 +164,38 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant
         }
     }
     __syncthreads();
+    // A CTA of the cluster has COLUMNS / splits columns to finish; the parts of each are written into its shared memory.
+    const int share = COLUMNS / a.splits;
+    if (a.splits > 1) cluster_wait();
     for (int i = threadIdx.x; i < M * T * COLUMNS; i += THREADS) {
         const int m = i / (T * COLUMNS), t = i / COLUMNS % T, col = i % COLUMNS;
         float s = 0.f;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) s += part[w][m][t * 8 + col % 8][col / 8];
-        sums[m][t][col] = s;
+        if (a.splits > 1) {
+            const int owner = col / share;
+            st_cluster(map_to_cta(smem_u32(&sums[m][t][(int)slice * share + col - owner * share]), (uint32_t)owner), s);
+        } else {
+            sums[m][t][col] = s;
+        }
     }
-    if (a.splits > 1) {
+    if (a.splits > 1) {  // after this nothing touches another CTA's memory
         cluster_arrive();
         cluster_wait();
     } else {
         __syncthreads();
     }
-    for (int i = (int)slice * THREADS + threadIdx.x; i < a.rows * COLUMNS; i += THREADS * a.splits) {
-        const int t = i / COLUMNS, col = i % COLUMNS;
-        if (c0 + col < a.N) {
+    for (int i = threadIdx.x; i < a.rows * share; i += THREADS) {
+        const int t = i / share, own = i - t * share;
+        const int64_t col = c0 + (int64_t)slice * share + own;
+        if (col < a.N) {
             float s[M];
 #pragma unroll
             for (int m = 0; m < M; ++m) {
                 s[m] = 0.f;
-                const uint32_t at = smem_u32(&sums[m][t][col]);
-                for (int r = 0; r < a.splits; ++r) s[m] += a.splits > 1 ? ld_cluster(map_to_cta(at, (uint32_t)r)) : sums[m][t][col];
+                for (int r = 0; r < a.splits; ++r) s[m] += sums[m][t][r * share + own];
             }
-            const int64_t at = (int64_t)t * a.N + c0 + col;
+            const int64_t at = (int64_t)t * a.N + col;
             if (GATED) {
                 float g[1] = {s[0]}, u[1] = {s[M - 1]}, h[1];
                 gated<F32>(a.gate, g, u, h);
@@ -196,10 +206,6 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant
                 static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(s[0]);
             }
         }
-    }
-    if (a.splits > 1) {  // nobody leaves while another reads its sums
-        cluster_arrive();
-        cluster_wait();
     }
 }
 
@@ -280,7 +286,7 @@ __global__ void __launch_bounds__(THREADS) few_rows_int8_kernel(const __grid_con
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
     pdl_launch_dependents();
-    constexpr int U = R == 1 ? 4 : 2;  // pieces of 512 bytes in flight a row
+    constexpr int U = R == 1 ? 8 : R == 2 ? 4 : 2;  // pieces of 512 bytes in flight a row
     const int64_t step = (int64_t)gridDim.x * WARPS * R;
     int64_t n0 = ((int64_t)blockIdx.x * WARPS + warp) * R;
     uint4 w[U][R];
@@ -386,22 +392,17 @@ cudaError_t launch_int8(const FewInt8Args& a, int64_t grid, cudaStream_t s, int6
     if (e != cudaSuccess) return e;
     return launch_clusters(kernel, grid, 1, (size_t)T * a.pitch, s, launches, a);
 }
-template <int QUANTIZE, int R>
-cudaError_t launch_int8_rows(const FewInt8Args& a, int64_t grid, cudaStream_t s, int64_t* launches) {
-    if (a.rows == 1) return launch_int8<QUANTIZE, R, 1>(a, grid, s, launches);
-    if (a.rows == 2) return launch_int8<QUANTIZE, R, 2>(a, grid, s, launches);
-    if (a.rows <= 4) return launch_int8<QUANTIZE, R, 4>(a, grid, s, launches);
-    return launch_int8<QUANTIZE, R, 8>(a, grid, s, launches);
-}
 template <int QUANTIZE>
 cudaError_t launch_int8_any(const FewInt8Args& a, int sm_count, cudaStream_t s, int64_t* launches) {
-    // four rows a warp where that still gives every SM a block: x is read from shared memory once for them
-    const int r = a.N >= (int64_t)sm_count * WARPS * 4 ? 4 : a.N >= (int64_t)sm_count * WARPS * 2 ? 2 : 1;
-    const int64_t needed = (a.N + WARPS * r - 1) / (WARPS * r), most = (int64_t)sm_count * 2;
+    // The more rows of x, the more rows of weights a warp has at a time, since x is read from shared memory once for them; eight loads
+    // are on their way in each case.  Blocks of 64 registers a thread: four to an SM.
+    const int r = a.rows <= 2 ? 1 : a.rows <= 4 ? 2 : 4;
+    const int64_t needed = (a.N + WARPS * r - 1) / (WARPS * r), most = (int64_t)sm_count * 4;
     const int64_t grid = needed < most ? needed : most;
-    if (r == 4) return launch_int8_rows<QUANTIZE, 4>(a, grid, s, launches);
-    if (r == 2) return launch_int8_rows<QUANTIZE, 2>(a, grid, s, launches);
-    return launch_int8_rows<QUANTIZE, 1>(a, grid, s, launches);
+    if (a.rows == 1) return launch_int8<QUANTIZE, 1, 1>(a, grid, s, launches);
+    if (a.rows == 2) return launch_int8<QUANTIZE, 1, 2>(a, grid, s, launches);
+    if (a.rows <= 4) return launch_int8<QUANTIZE, 2, 4>(a, grid, s, launches);
+    return launch_int8<QUANTIZE, 4, 8>(a, grid, s, launches);
 }
 
 }  // namespace

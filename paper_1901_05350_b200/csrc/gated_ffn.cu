@@ -35,8 +35,8 @@ struct LayoutArgs {
 
 template <bool F32>
 __global__ void __launch_bounds__(256) layout_kernel(const __grid_constant__ LayoutArgs args) {
-    ptx::pdl_launch_dependents();
     ptx::pdl_wait();
+    ptx::pdl_launch_dependents();
     int k = 0;
     while (k + 1 < args.count && (int64_t)blockIdx.x >= args.item[k + 1].first_block) ++k;
     const LayoutItem& it = args.item[k];
@@ -251,6 +251,7 @@ tfjsb_status tfjsb_gated_ffn(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, const void* x
     down.args.M = (int)s.T; down.args.N = (int)s.Do; down.args.K = (int)s.F;
     down.args.out[0] = y;
     down.args.out_pitch = s.Do;
+    down.args.early_b = 1;  // the weights, or their copy, which was made before the product before
     return run_product(ctx, down, stm);
 }
 
@@ -293,6 +294,24 @@ tfjsb_status tfjsb_gated_ffn_backprop(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, cons
     if ((st = run_layout(ctx, layout, s.planes == 3, stm)) != TFJSB_OK) return st;
     const int64_t plane = s.T * s.fp;
 
+    // The order leaves a kernel between those that write and read the same, so that each may start while the one before ends: the
+    // gradients of g and u, that of w_down (of h and dy alone), those of x and of the other weights.
+    __nv_bfloat16* grads = arena.take(s.grad_bytes);  // dg, then du: `planes` planes each
+    if (hidden_grads) {
+        Product dh;
+        dh.planes = s.planes;
+        dh.epilogue = EPI_GRAD;
+        dh.a = ody;
+        dh.b[0] = od;
+        dh.args.M = (int)s.T; dh.args.N = (int)s.F; dh.args.K = (int)s.Do;
+        dh.args.out[0] = grads;
+        dh.args.out_pitch = s.fp;
+        dh.args.out_plane = plane;
+        dh.args.z = const_cast<float*>(static_cast<const float*>(z));
+        dh.args.z_pitch = s.fp;
+        dh.args.gate = ffn->gate;
+        if ((st = run_product(ctx, dh, stm)) != TFJSB_OK) return st;
+    }
     if (dw_down) {
         Product p;
         p.planes = s.planes;
@@ -301,25 +320,9 @@ tfjsb_status tfjsb_gated_ffn_backprop(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, cons
         p.args.M = (int)s.F; p.args.N = (int)s.Do; p.args.K = (int)s.T;
         p.args.out[0] = dw_down;
         p.args.out_pitch = s.Do;
+        p.args.early_a = p.args.early_b = hidden_grads;
         if ((st = run_product(ctx, p, stm)) != TFJSB_OK) return st;
     }
-    if (!hidden_grads) return TFJSB_OK;
-
-    __nv_bfloat16* grads = arena.take(s.grad_bytes);  // dg, then du: `planes` planes each
-    Product dh;
-    dh.planes = s.planes;
-    dh.epilogue = EPI_GRAD;
-    dh.a = ody;
-    dh.b[0] = od;
-    dh.args.M = (int)s.T; dh.args.N = (int)s.F; dh.args.K = (int)s.Do;
-    dh.args.out[0] = grads;
-    dh.args.out_pitch = s.fp;
-    dh.args.out_plane = plane;
-    dh.args.z = const_cast<float*>(static_cast<const float*>(z));
-    dh.args.z_pitch = s.fp;
-    dh.args.gate = ffn->gate;
-    if ((st = run_product(ctx, dh, stm)) != TFJSB_OK) return st;
-
     if (dx) {
         Product p;
         p.planes = s.planes;
@@ -330,6 +333,8 @@ tfjsb_status tfjsb_gated_ffn_backprop(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, cons
         p.args.M = (int)s.T; p.args.N = (int)s.D; p.args.K = (int)s.F;
         p.args.out[0] = dx;
         p.args.out_pitch = s.D;
+        p.args.early_a = dw_down != nullptr;
+        p.args.early_b = 1;
         if ((st = run_product(ctx, p, stm)) != TFJSB_OK) return st;
     }
     if (dw_gate || dw_up) {
@@ -343,6 +348,8 @@ tfjsb_status tfjsb_gated_ffn_backprop(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, cons
         p.args.out[0] = dw_gate ? dw_gate : dw_up;
         p.args.out[1] = dw_up;
         p.args.out_pitch = s.F;
+        p.args.early_a = 1;
+        p.args.early_b = dw_down || dx;
         if ((st = run_product(ctx, p, stm)) != TFJSB_OK) return st;
     }
     return TFJSB_OK;

@@ -169,7 +169,7 @@ tfjsb_status check_product(tfjsb_ctx* ctx, const void* bt, const float* b_scale,
 }
 
 tfjsb_status product(tfjsb_ctx* ctx, const int8_t* a, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias, tfjsb_act act,
-                     void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, cudaStream_t s) {
+                     void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, bool quantized_before, cudaStream_t s) {
     if (few_rows_int8_supported(M, K))
         return few_rows_int8(ctx, 0, a, a_scale, bt, b_scale, bias, act, out, out_dtype == TFJSB_DTYPE_BF16, M, N, K, s);
     Product p;
@@ -187,6 +187,7 @@ tfjsb_status product(tfjsb_ctx* ctx, const int8_t* a, const float* a_scale, cons
     p.args.a_scale = a_scale;
     p.args.b_scale = b_scale;
     p.args.bias = bias;
+    p.args.early_b = quantized_before;  // the kernel before is the one that quantised A
     return run_product(ctx, p, s);
 }
 
@@ -227,7 +228,7 @@ tfjsb_status tfjsb_matmul_int8(tfjsb_ctx* ctx, const int8_t* a, const float* a_s
     if (!aligned(a, 16) || !aligned(a_scale, 16)) return fail(ctx, TFJSB_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
     const int64_t bytes = M * N * (out_dtype == TFJSB_DTYPE_F32 ? 4 : 2);
     if (overlap(out, bytes, a, M * K) || overlap(out, bytes, a_scale, 4 * M)) return fail(ctx, TFJSB_ERR_INVALID_ARG, "out overlaps an input");
-    return product(ctx, a, a_scale, bt, b_scale, bias, act, out, out_dtype, M, N, K, static_cast<cudaStream_t>(stream));
+    return product(ctx, a, a_scale, bt, b_scale, bias, act, out, out_dtype, M, N, K, false, static_cast<cudaStream_t>(stream));
 }
 
 int64_t tfjsb_dense_int8_workspace(int64_t M, int64_t K) {
@@ -258,7 +259,7 @@ tfjsb_status tfjsb_dense_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, 
     float* scale = reinterpret_cast<float*>(q + up256(M * up16(K)));
     const cudaError_t e = launch_quantize(dtype == TFJSB_DTYPE_F32, x, M, K, q, scale, s, &ctx->launches);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "quantize launch");
-    return product(ctx, q, scale, bt, b_scale, bias, act, out, out_dtype, M, N, up16(K), s);
+    return product(ctx, q, scale, bt, b_scale, bias, act, out, out_dtype, M, N, up16(K), true, s);
 }
 
 }  // extern "C"
