@@ -59,19 +59,19 @@ struct Product {
 };
 tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s);
 
-// Products of few rows (few_rows.cu).  h is fp32 [rows, N]; operands 16-byte aligned, of any sizes.
+// Products of few rows (few_rows.cu).  h is fp32 [rows, N]; operands 16-byte aligned, of any sizes.  FEW_ROWS at most; where the tensor
+// cores take the weights as they are stored (bfloat16) they are faster from three rows on (1024 x 4096: 2 rows 12 against 16 us, 4 rows 20 against
+// 16), where the weights would be split into planes first (fp32) they are not.
 constexpr int FEW_ROWS = 8;
+constexpr int few_rows_ffn(bool f32) { return f32 ? FEW_ROWS : 2; }
 tfjsb_status few_rows_gated(tfjsb_ctx* ctx, bool f32, const void* x, const void* w_gate, const void* w_up, int gate, float* h, int64_t rows, int64_t N,
                             int64_t K, cudaStream_t s);
 tfjsb_status few_rows_down(tfjsb_ctx* ctx, bool f32, const float* h, const void* w, void* y, int64_t rows, int64_t N, int64_t K, cudaStream_t s);
-// x_kind: 0 8-bit values [rows, K rounded up to 16] with a_scale, 1 bfloat16, 2 fp32.  The rows' 8-bit values have to fit shared memory.
-constexpr int FEW_INT8_BYTES = 98304;
-inline bool few_rows_int8_supported(int64_t rows, int64_t K) {
-    const int64_t held = rows <= 2 ? rows : rows <= 4 ? 4 : 8;
-    return rows <= FEW_ROWS && held * ((K + 15) / 16 * 16) <= FEW_INT8_BYTES;
-}
-tfjsb_status few_rows_int8(tfjsb_ctx* ctx, int x_kind, const void* x, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias,
-                           int act, void* out, bool out_bf16, int64_t rows, int64_t N, int64_t K, cudaStream_t s);
+// One row of 8-bit products.  x_kind: 0 8-bit values [K rounded up to 16] with a_scale, 1 bfloat16, 2 fp32.  (With two and four rows
+// 4096 x 4096 took 8.2 and 11.3 us this way, 8.3 for eight rows on the tensor cores.)
+constexpr int ROW_INT8_BYTES = 131072;  // of the largest K: the row's 8-bit values are in shared memory
+tfjsb_status row_int8(tfjsb_ctx* ctx, int x_kind, const void* x, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias, int act,
+                      void* out, bool out_bf16, int64_t N, int64_t K, cudaStream_t s);
 
 // The context's device is the current one while this lives: tensors say where they are, the caller's device may be another.
 struct OnDevice {

@@ -134,8 +134,9 @@ struct Maps {
     CUtensorMap out[2];  // results that are stored from shared memory
 };
 
-// Shared memory of an epilogue warp: a chunk of 32 rows of a result on its way out, rows of 64 bytes.
-template <int P, int EPI> constexpr int SLAB_BYTES = P == 1 && (EPI == EPI_STORE || EPI == EPI_SCALE) ? 2048 : 0;
+// Shared memory of an epilogue warp: a chunk of 32 rows of a result on its way out, rows of 64 bytes, or g and u of 32 rows and 16
+// columns on their way in.
+template <int P, int EPI> constexpr int SLAB_BYTES = P == 3 || EPI == EPI_GATED ? 0 : EPI == EPI_GRAD ? 4096 : 2048;
 
 // 16-byte piece j of row r of a chunk whose rows are B bytes, in the swizzle of B bytes.
 template <int B>
@@ -258,6 +259,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
     __shared__ __align__(8) uint64_t bar_acc_empty[2];      // CG = 2: used in the even CTA only
     __shared__ __align__(8) uint64_t bar_drain;
     constexpr int SLAB = SLAB_BYTES<P, EPI>;
+    __shared__ __align__(8) uint64_t bar_z[EPI == EPI_GRAD && P == 1 ? EPI_WARPS : 1];
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag_s;
 
@@ -291,6 +293,8 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
             mbar_init(smem_u32(&bar_acc_empty[s]), EPI_WARPS * CG);
         }
         mbar_init(smem_u32(&bar_drain), 1);
+        if (EPI == EPI_GRAD && P == 1)
+            for (int i = 0; i < EPI_WARPS; ++i) mbar_init(smem_u32(&bar_z[i]), 1);
         abort_flag_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
@@ -560,6 +564,8 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
         const uint32_t pitch = (uint32_t)(block_n + 4) * 4u;  // of a partial tile's row: consecutive rows start 4 banks apart
         const int ew = warp - 2;
         const uint32_t slab = stage_base + (uint32_t)stages * stage_bytes + (uint32_t)(ew * SLAB);
+        uint32_t z_phase = 0;
+        int z_out = 0;  // a copy into the slab is on its way
         int acc = 0;
         uint32_t phases = 0;  // of the accumulators, a bit each
         bool ok = true;
@@ -613,12 +619,18 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                     const int64_t row0 = m0 + u * (CG * ROWS) + quad * 32, row = row0 + lane;
                     const bool rows_live = row0 < args.M;
                     const float row_scale = EPI == EPI_SCALE && row < args.M ? load_global(args.a_scale + row) : 0.f;
-                    float g8[8], u8[8];  // EPI_GRAD: g and u of the next eight columns, on their way while eight are worked on
+                    // EPI_GRAD: g and u of a chunk's 32 rows and 16 columns, 4 KiB in one piece, on their way while the chunk before is worked on.
+                    // (Loads into registers leave room for half as many bytes on their way: 4096 x 2048 x 8192 122 us.)
                     auto fetch = [&](int col) {
-                        if (EPI == EPI_GRAD && rows_live && col < args.N) {  // rows are filled up to whole blocks
-                            load_f32(z_at(args, row, col, 0), g8, 8);
-                            load_f32(z_at(args, row, col, 1), u8, 8);
+                        if (EPI != EPI_GRAD || !rows_live || col >= args.N) return;
+                        const float* from = z_at(args, row0, col, 0);
+                        const uint32_t bar = smem_u32(&bar_z[EPI == EPI_GRAD ? ew : 0]);
+                        if (elected) {
+                            mbar_arrive_expect_tx(bar, 4096u);
+                            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(slab), "l"(from),
+                                         "r"(4096u), "r"(bar) : "memory");
                         }
+                        z_out = 1;
                     };
                     if (part < n_chunks) fetch(n0 + part * chunk);
                     if (!(ok = wait_acc())) break;
@@ -638,28 +650,49 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                             if (ch + PARTS >= n_chunks) release_acc();
                             if (!rows_live || col >= args.N) continue;
                             float out[EPI == EPI_GATED ? 1 : 2][16];
+                            if constexpr (EPI == EPI_GATED) {
 #pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                float v[8], w[8], x[8];
+                                for (int j = 0; j < 2; ++j) {
+                                    float g[8], u[8], v[8];
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(first[j][i]);
-                                if constexpr (EPI == EPI_GATED) {
-#pragma unroll
-                                    for (int i = 0; i < 8; ++i) w[i] = __uint_as_float(second[j][i]);
+                                    for (int i = 0; i < 8; ++i) { g[i] = __uint_as_float(first[j][i]); u[i] = __uint_as_float(second[j][i]); }
                                     if (args.z && col + 8 * j < args.N) {
-                                        store_f32(z_at(args, row, col + 8 * j, 0), v, 8);
-                                        store_f32(z_at(args, row, col + 8 * j, 1), w, 8);
+                                        store_f32(z_at(args, row, col + 8 * j, 0), g, 8);
+                                        store_f32(z_at(args, row, col + 8 * j, 1), u, 8);
                                     }
-                                    gated<false>(args.gate, v, w, x);
+                                    gated<false>(args.gate, g, u, v);
 #pragma unroll
-                                    for (int i = 0; i < 8; ++i) out[0][8 * j + i] = x[i];
-                                } else {
+                                    for (int i = 0; i < 8; ++i) out[0][8 * j + i] = v[i];
+                                }
+                            } else {
+                                const bool got = bounded_wait(smem_u32(&bar_z[ew]), z_phase, abort_flag);
+                                if (!__all_sync(0xffffffffu, got)) {
+                                    if (lane == 0) give_up(abort_flag, args.dev_status, DEV_STATUS_TIMEOUT_EPILOGUE);
+                                    ok = false;
+                                    break;
+                                }
+                                z_phase ^= 1u;
+                                z_out = 0;
+                                float g[2][8], u[2][8];
 #pragma unroll
-                                    for (int i = 0; i < 8; ++i) { w[i] = g8[i]; x[i] = u8[i]; }
-                                    const int next = j == 0 ? col + 8 : ch + PARTS < n_chunks ? col + PARTS * 16 : args.N;
-                                    fetch(next);
-                                    float du[8];
-                                    gated_gradient<false>(args.gate, w, x, v, du);
+                                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                    for (int i = 0; i < 8; i += 4) {
+                                        const float4 x = tile::lds4(slab + (uint32_t)(j * 2048 + lane * 32 + i * 4)), y = tile::lds4(slab + (uint32_t)(j * 2048 + 1024 + lane * 32 + i * 4));
+                                        g[j][i] = x.x; g[j][i + 1] = x.y; g[j][i + 2] = x.z; g[j][i + 3] = x.w;
+                                        u[j][i] = y.x; u[j][i + 1] = y.y; u[j][i + 2] = y.z; u[j][i + 3] = y.w;
+                                    }
+                                // All have read it, and have their values, before the next copy overwrites it.  (Without the fence the
+                                // compiler moved half of the reads behind the copy's issue, in one of the instances.)
+                                fence_async_smem();
+                                __syncwarp();
+                                if (ch + PARTS < n_chunks) fetch(col + PARTS * 16);
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    float v[8], du[8];
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(first[j][i]);
+                                    gated_gradient<false>(args.gate, g[j], u[j], v, du);
 #pragma unroll
                                     for (int i = 0; i < 8; ++i) { out[0][8 * j + i] = v[i]; out[EPI == EPI_GRAD ? 1 : 0][8 * j + i] = du[i]; }
                                 }
@@ -792,6 +825,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                 }
             }
         }
+        if (EPI == EPI_GRAD && P == 1 && z_out) drain(smem_u32(&bar_z[EPI == EPI_GRAD && P == 1 ? ew : 0]), z_phase, args.dev_status);  // after a time-out
         if (elected) tma_store_wait_all();
         __syncwarp();
     }
@@ -927,7 +961,7 @@ int64_t tiles_of(const Product& p, int cg, int block_n, int subs = 1) {
 
 // Estimated cycles, fitted to clocks read in the kernel (at about 1.9 GHz) and to whole products:
 //   - a k-block takes what its MMAs take (2 cycles a column and plane product) or what an SM can fetch (50 bytes a cycle), whichever
-//     is longer; a pair with two parts fetches three tiles for two, a pair half of B, single CTAs everything;
+//     is longer, but not less than issuing its MMAs takes (390); a pair with two parts fetches three tiles for two, a pair half of B, single CTAs everything;
 //   - the first k-block arrives 3400 cycles after the start (4200 in a pair), an epilogue warp takes 900 to 1950 cycles for a chunk;
 //   - with one part a tile the epilogue runs beside the next tile's K loop, with two it holds up the next tile for most of the time it takes;
 //   - slices cost two cluster barriers and a round trip for each share of the tile that a thread adds.
@@ -937,16 +971,17 @@ double cost(const Product& p, const Shape& c, int sm_count) {
     const double rows = a.M < ROWS ? a.M : ROWS;
     auto k_block = [&](int subs) {
         const double fetch = p.planes * 128. * (rows * subs + c.block_n / c.cg) / 50, mma = 2.16 * c.block_n * subs * (p.planes == 3 ? 6 : 1);
-        return fetch > mma ? fetch : mma;
+        const double longer = fetch > mma ? fetch : mma, issue = 390. * (p.planes == 3 ? 4 : 1);
+        return longer > issue ? longer : issue;
     };
     const double main = own_kb * k_block(c.subs), first = c.cg == 2 ? 4200 : 3400;
     const int columns = p.epilogue == EPI_GATED ? c.block_n / 2 : c.block_n;
-    const double chunk = p.epilogue == EPI_STORE ? 900. / 32 : p.epilogue == EPI_SCALE ? 1300. / 32 : p.epilogue == EPI_GRAD ? 1800. / 16 : a.z ? 1400. / 16 : 1200. / 16;
+    const double chunk = p.epilogue == EPI_STORE ? 900. / 32 : p.epilogue == EPI_SCALE ? 3000. / 32 : p.epilogue == EPI_GRAD ? 1800. / 16 : a.z ? 1400. / 16 : 1200. / 16;
     const double epilogue = columns / 4 * chunk * (p.planes == 3 ? 2.5 : 1);
     const int64_t tiles = tiles_of(p, c.cg, c.block_n, c.subs), slots = sm_count / c.cg;
     if (c.splits > 1) {
         const int64_t shares = (int64_t)rows * (columns / 8), each = 32 * EPI_WARPS * c.splits;
-        return first + main + 3200 + (double)((shares + each - 1) / each) * 2000;
+        return first + main + 4000 + (double)((shares + each - 1) / each) * 1500;
     }
     const int64_t rounds = tiles / slots, rest = tiles % slots;
     if (c.subs == 2) {
@@ -1046,7 +1081,7 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     a.dev_status = ctx->dev_status;
     const int own_n = c.block_n / c.cg;
     const int stage_bytes = p.planes * (c.subs * A_BYTES + own_n * 128);
-    const int slabs = EPI_WARPS * (p.planes == 1 && (p.epilogue == EPI_STORE || p.epilogue == EPI_SCALE) ? SLAB_BYTES<1, EPI_STORE> : 0);
+    const int slabs = EPI_WARPS * (p.planes == 3 || p.epilogue == EPI_GATED ? 0 : p.epilogue == EPI_GRAD ? SLAB_BYTES<1, EPI_GRAD> : SLAB_BYTES<1, EPI_STORE>);
     const int stages = (tile::SMEM_LIMIT - 2048 - 1024 - slabs) / stage_bytes;
     a.stages = stages < MAX_STAGES ? stages : MAX_STAGES;
     const size_t smem = 1024 + (size_t)a.stages * stage_bytes + slabs;

@@ -1,13 +1,13 @@
 // Products of few rows with large weights, on CUDA cores: the dense layers of transformer blocks when they serve single tokens.
 //
-// With up to eight rows nothing but reading the weights costs time (a byte of them is used in 1 to 8 multiply-adds), so what counts is
+// With a few rows nothing but reading the weights costs time (a byte of them is used in 1 to 8 multiply-adds), so what counts is
 // that every SM has enough loads in flight and that the launches are short.  Each weight is read once, 16 bytes a load, all rows are
 // multiplied with it, and long sums are cut among the threads, the warps and the CTAs of a cluster, whose parts are added in a fixed
 // order through shared and distributed shared memory.
 //
 //   matrices [K, N] (the gated block): a block has 64 columns, a thread 8 of them and every 32nd k; K is cut among the CTAs of a cluster
-//   matrices [N, K] of 8-bit integers: a warp has 1 to 4 rows of weights, a lane 16 bytes of each 512; the rows of x are quantised, or copied, into
-//   shared memory by every block
+//   matrices [N, K] of 8-bit integers, one row of x: a warp has a row of weights, a lane 16 bytes of each 512; the row of x is quantised, or
+//   copied, into shared memory by every block
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -83,7 +83,7 @@ struct FewArgs {
 template <bool F32, bool X32, bool GATED, int T, bool VECTOR>
 __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant__ FewArgs a) {
     constexpr int M = GATED ? 2 : 1;
-    constexpr int U = T >= 8 ? 4 : 8;  // rows of weights in flight a thread and matrix
+    constexpr int U = T >= 8 || (GATED && T <= 2) ? 4 : 8;  // rows of weights in flight a thread and matrix
     extern __shared__ float xs[];      // [k][T] of this slice, a chunk at a time
     __shared__ float part[WARPS][M][T * 8][8];
     __shared__ float sums[M][T][COLUMNS];  // [slice][column of this CTA's share]: every CTA of the cluster writes its slice's part
@@ -96,13 +96,19 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant
     float acc[M][T][8] = {};
     if (a.splits > 1) cluster_arrive();  // "has begun", which the others wait for before they write here
     Eight<F32> w[M][U];
-    auto fetch = [&](int k0, int count, int k) {
+    auto fetch_half = [&](int k0, int count, int k, int half) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int v = 0; v < U / 2; ++v) {
+            const int u = half * (U / 2) + v;
             if (k + u * K_LANES < count && left > 0) {
                 w[0][u].template load<VECTOR>(a.w0, k0 + k + u * K_LANES, a.N, c, left);
                 if (GATED) w[M - 1][u].template load<VECTOR>(a.w1, k0 + k + u * K_LANES, a.N, c, left);
             }
+        }
+    };
+    auto fetch = [&](int k0, int count, int k) {
+        fetch_half(k0, count, k, 0);
+        fetch_half(k0, count, k, 1);
     };
     // The second kernel of a block follows the first, which writes no weights and lets this one start once everything before it is
     // done: its first weights are on their way while the first kernel runs.
@@ -126,22 +132,28 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant
         }
         __syncthreads();
         for (int k = k_lane; k < count; k += U * K_LANES) {
+            // one half is used while the other, and then its own successor, is on its way
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (k + u * K_LANES < count && left > 0) {
-                    float x[T];
+            for (int half = 0; half < 2; ++half) {
 #pragma unroll
-                    for (int t = 0; t < T; ++t) x[t] = xs[(k + u * K_LANES) * T + t];
+                for (int v = 0; v < U / 2; ++v) {
+                    const int u = half * (U / 2) + v;
+                    if (k + u * K_LANES < count && left > 0) {
+                        float x[T];
 #pragma unroll
-                    for (int m = 0; m < M; ++m)
+                        for (int t = 0; t < T; ++t) x[t] = xs[(k + u * K_LANES) * T + t];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float v = w[m][u][i];
+                        for (int m = 0; m < M; ++m)
 #pragma unroll
-                            for (int t = 0; t < T; ++t) acc[m][t][i] = fmaf(x[t], v, acc[m][t][i]);
-                        }
+                            for (int i = 0; i < 8; ++i) {
+                                const float value = w[m][u][i];
+#pragma unroll
+                                for (int t = 0; t < T; ++t) acc[m][t][i] = fmaf(x[t], value, acc[m][t][i]);
+                            }
+                    }
                 }
-            if (k + U * K_LANES < count) fetch(k0, count, k + U * K_LANES);
+                if (k + U * K_LANES < count) fetch_half(k0, count, k + U * K_LANES, half);
+            }
         }
     }
 
@@ -250,159 +262,139 @@ cudaError_t launch_few(const FewArgs& a, bool vector, int64_t grid, cudaStream_t
 template <bool F32, bool X32, bool GATED>
 tfjsb_status few(tfjsb_ctx* ctx, const void* x, const void* w0, const void* w1, int gate, void* out, int64_t rows, int64_t N, int64_t K, cudaStream_t s) {
     FewArgs a = {x, w0, w1, out, N, (int)K, (int)rows, 0, 1, gate};
-    // As many slices as give each SM two blocks at most and each thread at least 4 rows of weights.
+    // As many slices as give each SM two blocks at most (three of the gated product of one or two rows, whose blocks are smaller) and each
+    // thread at least 4 rows of weights.
     const int64_t blocks = (N + COLUMNS - 1) / COLUMNS;
-    while (a.splits < 8 && blocks * a.splits * 2 <= 2 * ctx->sm_count && K / (a.splits * 2) >= 4 * K_LANES) a.splits *= 2;
+    const int64_t most = (int64_t)(GATED && rows <= 2 ? 3 : 2) * ctx->sm_count;
+    while (a.splits < 8 && blocks * a.splits * 2 <= most && K / (a.splits * 2) >= 4 * K_LANES) a.splits *= 2;
     a.k_per_slice = (int)((K + a.splits - 1) / a.splits);
     const bool vector = N % 8 == 0;  // pointers are 16-byte aligned
     const int64_t grid = blocks * a.splits;
     if (grid >= (1LL << 31)) return fail(ctx, TFJSB_ERR_UNSUPPORTED, "too many columns");
     cudaError_t e;
     if (rows == 1) e = launch_few<F32, X32, GATED, 1>(a, vector, grid, s, &ctx->launches);
-    else if (rows == 2) e = launch_few<F32, X32, GATED, 2>(a, vector, grid, s, &ctx->launches);
-    else if (rows <= 4) e = launch_few<F32, X32, GATED, 4>(a, vector, grid, s, &ctx->launches);
-    else e = launch_few<F32, X32, GATED, 8>(a, vector, grid, s, &ctx->launches);
+    else if (!F32 || rows == 2) e = launch_few<F32, X32, GATED, 2>(a, vector, grid, s, &ctx->launches);  // bfloat16: two rows at most
+    else if (rows <= 4) e = launch_few<F32, X32, GATED, F32 ? 4 : 2>(a, vector, grid, s, &ctx->launches);
+    else e = launch_few<F32, X32, GATED, F32 ? 8 : 2>(a, vector, grid, s, &ctx->launches);
     return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "few rows launch");
 }
 
 // ---- 8-bit weights -------------------------------------------------------------------------------------------
 
 struct FewInt8Args {
-    const void* x;         // QUANTIZE: [rows, K] values; otherwise [rows, pitch] 8-bit
+    const void* x;         // QUANTIZE: K values; otherwise [pitch] 8-bit
     const float* a_scale;  // not with QUANTIZE
     const int8_t* bt;      // [N, pitch]
     const float *b_scale, *bias;
     void* out;
     int64_t N;
-    int K, pitch, rows, act, out_bf16;
+    int K, pitch, act, out_bf16;
 };
 
-// QUANTIZE: 0 x is 8-bit already, 1 bfloat16, 2 fp32.  R weight rows a warp at a time, T rows of x.
-template <int QUANTIZE, int R, int T>
+// One row of x.  QUANTIZE: 0 x is 8-bit already, 1 bfloat16, 2 fp32.
+template <int QUANTIZE>
 __global__ void __launch_bounds__(THREADS) few_rows_int8_kernel(const __grid_constant__ FewInt8Args a) {
-    extern __shared__ __align__(16) int8_t q[];  // [T][pitch]
-    __shared__ float largest[T][WARPS];
-    __shared__ float scale[T];
+    extern __shared__ __align__(16) int8_t q[];  // [pitch]
+    __shared__ float largest[WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
     pdl_launch_dependents();
-    constexpr int U = R == 1 ? 8 : R == 2 ? 4 : 2;  // pieces of 512 bytes in flight a row
-    const int64_t step = (int64_t)gridDim.x * WARPS * R;
-    int64_t n0 = ((int64_t)blockIdx.x * WARPS + warp) * R;
-    uint4 w[U][R];
-    auto fetch = [&](int64_t n, int k) {
+    constexpr int U = 8;     // pieces of 512 bytes of a row of weights in flight a warp
+    constexpr int HELD = 2;  // groups of eight values of x that a thread holds between the maximum and the rounding
+    const int64_t step = (int64_t)gridDim.x * WARPS;
+    int64_t n = (int64_t)blockIdx.x * WARPS + warp;
+    uint4 w[U];
+    auto fetch = [&](int64_t row, int k) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                w[u][r] = make_uint4(0u, 0u, 0u, 0u);
-                if (n + r < a.N && k + u * 512 < a.pitch) w[u][r] = ld_weights(a.bt + (n + r) * a.pitch + k + u * 512);
-            }
+        for (int u = 0; u < U; ++u) {
+            w[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (row < a.N && k + u * 512 < a.pitch) w[u] = ld_weights(a.bt + row * a.pitch + k + u * 512);
+        }
     };
-    if (n0 < a.N) fetch(n0, lane * 16);  // on its way while x is laid out
+    fetch(n, lane * 16);  // on its way while x is laid out
 
+    float scale;
     if (QUANTIZE == 0) {
-        for (int i = threadIdx.x * 16; i < T * a.pitch; i += THREADS * 16) {
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (i / a.pitch < a.rows) v = *reinterpret_cast<const uint4*>(static_cast<const int8_t*>(a.x) + i);
-            *reinterpret_cast<uint4*>(q + i) = v;
-        }
-        if (threadIdx.x < T) scale[threadIdx.x] = threadIdx.x < a.rows ? load_global(a.a_scale + threadIdx.x) : 0.f;
-        __syncthreads();
+        for (int i = threadIdx.x * 16; i < a.pitch; i += THREADS * 16)
+            *reinterpret_cast<uint4*>(q + i) = load_global(reinterpret_cast<const uint4*>(static_cast<const int8_t*>(a.x) + i));
+        scale = load_global(a.a_scale);
     } else {
-#pragma unroll 1
-        for (int t = 0; t < T; ++t) {
-            float m = 0.f;
-            if (t < a.rows)
-                for (int k = threadIdx.x * 8; k < a.K; k += THREADS * 8) {
-                    float v[8];
-                    values8<QUANTIZE == 2>(a.x, (int64_t)t * a.K + k, a.K - k < 8 ? a.K - k : 8, v);
+        auto left_at = [&](int k) { return a.K - k < 8 ? a.K - k : 8; };
+        float v[HELD][8], m = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(v[e]));
-                }
+        for (int j = 0; j < HELD; ++j) {
+            const int k = (j * THREADS + threadIdx.x) * 8;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-            if (lane == 0) largest[t][warp] = m;
+            for (int e = 0; e < 8; ++e) v[j][e] = 0.f;
+            if (k < a.K) values8<QUANTIZE == 2>(a.x, k, left_at(k), v[j]);
         }
-        __syncthreads();
-#pragma unroll 1
-        for (int t = 0; t < T; ++t) {
-            float m = largest[t][0];
 #pragma unroll
-            for (int i = 1; i < WARPS; ++i) m = max_nan(m, largest[t][i]);
-            const RowScale rs = row_scale(m);
-            if (threadIdx.x == 0) scale[t] = m / 127.f;
-            for (int k = threadIdx.x * 8; k < a.pitch; k += THREADS * 8) {
-                float v[8] = {};
-                if (t < a.rows && k < a.K) values8<QUANTIZE == 2>(a.x, (int64_t)t * a.K + k, a.K - k < 8 ? a.K - k : 8, v);
-                *reinterpret_cast<uint2*>(q + t * a.pitch + k) = quantize8<QUANTIZE == 2>(v, rs);
-            }
+        for (int j = 0; j < HELD; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(v[j][e]));
+        for (int k = (HELD * THREADS + threadIdx.x) * 8; k < a.K; k += THREADS * 8) {
+            float more[8];
+            values8<QUANTIZE == 2>(a.x, k, left_at(k), more);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(more[e]));
         }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (lane == 0) largest[warp] = m;
         __syncthreads();
+        m = largest[0];
+#pragma unroll
+        for (int i = 1; i < WARPS; ++i) m = max_nan(m, largest[i]);
+        const RowScale rs = row_scale(m);
+        scale = m / 127.f;
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) {
+            const int k = (j * THREADS + threadIdx.x) * 8;
+            if (k < a.pitch) *reinterpret_cast<uint2*>(q + k) = quantize8<QUANTIZE == 2>(v[j], rs);
+        }
+        for (int k = (HELD * THREADS + threadIdx.x) * 8; k < a.pitch; k += THREADS * 8) {
+            float more[8] = {};
+            if (k < a.K) values8<QUANTIZE == 2>(a.x, k, left_at(k), more);
+            *reinterpret_cast<uint2*>(q + k) = quantize8<QUANTIZE == 2>(more, rs);
+        }
     }
+    __syncthreads();
 
-    for (; n0 < a.N; n0 += step) {
-        int acc[R][T] = {};
+    for (; n < a.N; n += step) {
+        int sum = 0;
         for (int k = lane * 16; k < a.pitch; k += U * 512) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (k + u * 512 < a.pitch) {
-#pragma unroll
-                    for (int t = 0; t < T; ++t) {
-                        const int4 v = *reinterpret_cast<const int4*>(q + t * a.pitch + k + u * 512);
-#pragma unroll
-                        for (int r = 0; r < R; ++r) {
-                            acc[r][t] = __dp4a((int)w[u][r].x, v.x, acc[r][t]);
-                            acc[r][t] = __dp4a((int)w[u][r].y, v.y, acc[r][t]);
-                            acc[r][t] = __dp4a((int)w[u][r].z, v.z, acc[r][t]);
-                            acc[r][t] = __dp4a((int)w[u][r].w, v.w, acc[r][t]);
-                        }
-                    }
+                    const int4 x = *reinterpret_cast<const int4*>(q + k + u * 512);
+                    sum = __dp4a((int)w[u].x, x.x, sum);
+                    sum = __dp4a((int)w[u].y, x.y, sum);
+                    sum = __dp4a((int)w[u].z, x.z, sum);
+                    sum = __dp4a((int)w[u].w, x.w, sum);
                 }
-            // the loop's condition differs from lane to lane in the last piece, and so does the next load
-            if (k + U * 512 < a.pitch) fetch(n0, k + U * 512);
+            if (k + U * 512 < a.pitch) fetch(n, k + U * 512);  // the last pieces differ from lane to lane
         }
         __syncwarp();
-        if (n0 + step < a.N) fetch(n0 + step, lane * 16);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int t = 0; t < T; ++t) acc[r][t] = __reduce_add_sync(0xffffffffu, acc[r][t]);
-        if (lane < R * T) {
-            const int r = lane / T, t = lane - r * T;
-            int sum = 0;
-#pragma unroll
-            for (int i = 0; i < R * T; ++i) sum = i == lane ? acc[i / T][i % T] : sum;
-            const int64_t n = n0 + r;
-            if (n < a.N && t < a.rows) {
-                float v = (float)sum * scale[t] * load_global(a.b_scale + n);
-                if (a.bias) v += load_global(a.bias + n);
-                v = apply_act(v, a.act);
-                if (a.out_bf16) static_cast<__nv_bfloat16*>(a.out)[t * a.N + n] = __float2bfloat16_rn(v);
-                else static_cast<float*>(a.out)[t * a.N + n] = v;
-            }
+        fetch(n + step, lane * 16);
+        sum = __reduce_add_sync(0xffffffffu, sum);
+        if (lane == 0) {
+            // as the tensor-core product's epilogue does it, to the bit
+            float v = fmaf((float)sum * scale, load_global(a.b_scale + n), a.bias ? load_global(a.bias + n) : 0.f);
+            v = apply_act(v, a.act);
+            if (a.out_bf16) static_cast<__nv_bfloat16*>(a.out)[n] = __float2bfloat16_rn(v);
+            else static_cast<float*>(a.out)[n] = v;
         }
     }
 }
 
-template <int QUANTIZE, int R, int T>
-cudaError_t launch_int8(const FewInt8Args& a, int64_t grid, cudaStream_t s, int64_t* launches) {
-    auto* kernel = &few_rows_int8_kernel<QUANTIZE, R, T>;
-    const cudaError_t e = smem_attr_once(reinterpret_cast<const void*>(kernel), FEW_INT8_BYTES);
-    if (e != cudaSuccess) return e;
-    return launch_clusters(kernel, grid, 1, (size_t)T * a.pitch, s, launches, a);
-}
 template <int QUANTIZE>
-cudaError_t launch_int8_any(const FewInt8Args& a, int sm_count, cudaStream_t s, int64_t* launches) {
-    // The more rows of x, the more rows of weights a warp has at a time, since x is read from shared memory once for them; eight loads
-    // are on their way in each case.  Blocks of 64 registers a thread: four to an SM.
-    const int r = a.rows <= 2 ? 1 : a.rows <= 4 ? 2 : 4;
-    const int64_t needed = (a.N + WARPS * r - 1) / (WARPS * r), most = (int64_t)sm_count * 4;
-    const int64_t grid = needed < most ? needed : most;
-    if (a.rows == 1) return launch_int8<QUANTIZE, 1, 1>(a, grid, s, launches);
-    if (a.rows == 2) return launch_int8<QUANTIZE, 1, 2>(a, grid, s, launches);
-    if (a.rows <= 4) return launch_int8<QUANTIZE, 2, 4>(a, grid, s, launches);
-    return launch_int8<QUANTIZE, 4, 8>(a, grid, s, launches);
+cudaError_t launch_int8(const FewInt8Args& a, int sm_count, cudaStream_t s, int64_t* launches) {
+    auto* kernel = &few_rows_int8_kernel<QUANTIZE>;
+    const cudaError_t e = smem_attr_once(reinterpret_cast<const void*>(kernel), ROW_INT8_BYTES);
+    if (e != cudaSuccess) return e;
+    // a row of weights a warp; blocks of 64 registers a thread are four to an SM
+    const int64_t needed = (a.N + WARPS - 1) / WARPS, most = (int64_t)sm_count * 4;
+    return launch_clusters(kernel, needed < most ? needed : most, 1, (size_t)a.pitch, s, launches, a);
 }
 
 }  // namespace
@@ -415,13 +407,13 @@ tfjsb_status few_rows_down(tfjsb_ctx* ctx, bool f32, const float* h, const void*
     return f32 ? few<true, true, false>(ctx, h, w, nullptr, 0, y, rows, N, K, s) : few<false, true, false>(ctx, h, w, nullptr, 0, y, rows, N, K, s);
 }
 
-tfjsb_status few_rows_int8(tfjsb_ctx* ctx, int x_kind, const void* x, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias,
-                           int act, void* out, bool out_bf16, int64_t rows, int64_t N, int64_t K, cudaStream_t s) {
-    const FewInt8Args a = {x, a_scale, bt, b_scale, bias, out, N, (int)K, (int)((K + 15) / 16 * 16), (int)rows, act, out_bf16 ? 1 : 0};
-    const cudaError_t e = x_kind == 0   ? launch_int8_any<0>(a, ctx->sm_count, s, &ctx->launches)
-                          : x_kind == 1 ? launch_int8_any<1>(a, ctx->sm_count, s, &ctx->launches)
-                                        : launch_int8_any<2>(a, ctx->sm_count, s, &ctx->launches);
-    return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "few rows launch");
+tfjsb_status row_int8(tfjsb_ctx* ctx, int x_kind, const void* x, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias, int act,
+                      void* out, bool out_bf16, int64_t N, int64_t K, cudaStream_t s) {
+    const FewInt8Args a = {x, a_scale, bt, b_scale, bias, out, N, (int)K, (int)((K + 15) / 16 * 16), act, out_bf16 ? 1 : 0};
+    const cudaError_t e = x_kind == 0   ? launch_int8<0>(a, ctx->sm_count, s, &ctx->launches)
+                          : x_kind == 1 ? launch_int8<1>(a, ctx->sm_count, s, &ctx->launches)
+                                        : launch_int8<2>(a, ctx->sm_count, s, &ctx->launches);
+    return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "8-bit row launch");
 }
 
 }  // namespace dense

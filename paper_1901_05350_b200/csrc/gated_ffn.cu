@@ -100,7 +100,7 @@ tfjsb_status sizes_of(const tfjsb_ffn* f, Sizes* s, std::string* why) {
     s->z_bytes = up256((s->T + 31) / 32 * 32 * s->fp * 8);  // whole blocks of 32 rows
     s->grad_bytes = up256(s->T * s->fp * 2 * e);
     const int64_t weights = (s->repack_x ? s->x_bytes : 0) + (s->repack_up ? 2 * s->w_bytes : 0) + (s->repack_down ? s->wd_bytes : 0);
-    s->few = s->T <= FEW_ROWS ? up256(s->T * s->F * 4) : 0;
+    s->few = s->T <= few_rows_ffn(f32) ? up256(s->T * s->F * 4) : 0;
     s->forward = weights + s->h_bytes > s->few ? weights + s->h_bytes : s->few;
     s->backward = weights + (s->repack_dy ? s->dy_bytes : 0) + s->grad_bytes;
     return TFJSB_OK;
@@ -214,7 +214,7 @@ tfjsb_status tfjsb_gated_ffn(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, const void* x
                        {w_down, s.F * s.Do * size, "w_down"}};
     if ((st = check_ranges(ctx, r, 8, 4, 6u)) != TFJSB_OK) return st;
     const cudaStream_t stm = static_cast<cudaStream_t>(stream);
-    if (!h && s.T <= FEW_ROWS) {
+    if (!h && s.T <= few_rows_ffn(s.planes == 3)) {
         float* few = static_cast<float*>(workspace);
         if ((st = few_rows_gated(ctx, s.planes == 3, x, w_gate, w_up, ffn->gate, few, s.T, s.F, s.D, stm)) != TFJSB_OK) return st;
         return few_rows_down(ctx, s.planes == 3, few, w_down, y, s.T, s.Do, s.F, stm);

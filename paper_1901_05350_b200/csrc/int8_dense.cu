@@ -170,8 +170,7 @@ tfjsb_status check_product(tfjsb_ctx* ctx, const void* bt, const float* b_scale,
 
 tfjsb_status product(tfjsb_ctx* ctx, const int8_t* a, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias, tfjsb_act act,
                      void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, bool quantized_before, cudaStream_t s) {
-    if (few_rows_int8_supported(M, K))
-        return few_rows_int8(ctx, 0, a, a_scale, bt, b_scale, bias, act, out, out_dtype == TFJSB_DTYPE_BF16, M, N, K, s);
+    if (M == 1) return row_int8(ctx, 0, a, a_scale, bt, b_scale, bias, act, out, out_dtype == TFJSB_DTYPE_BF16, N, K, s);
     Product p;
     p.kind = KIND_INT8;
     p.epilogue = EPI_SCALE;
@@ -253,8 +252,7 @@ tfjsb_status tfjsb_dense_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, 
         overlap(workspace, needed, bt, N * up16(K)) || overlap(workspace, needed, b_scale, 4 * N) || overlap(workspace, needed, bias, 4 * N))
         return fail(ctx, TFJSB_ERR_INVALID_ARG, "out or the workspace overlaps another argument");
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (few_rows_int8_supported(M, K))
-        return few_rows_int8(ctx, dtype == TFJSB_DTYPE_F32 ? 2 : 1, x, nullptr, bt, b_scale, bias, act, out, out_dtype == TFJSB_DTYPE_BF16, M, N, K, s);
+    if (M == 1) return row_int8(ctx, dtype == TFJSB_DTYPE_F32 ? 2 : 1, x, nullptr, bt, b_scale, bias, act, out, out_dtype == TFJSB_DTYPE_BF16, N, K, s);
     int8_t* q = static_cast<int8_t*>(workspace);
     float* scale = reinterpret_cast<float*>(q + up256(M * up16(K)));
     const cudaError_t e = launch_quantize(dtype == TFJSB_DTYPE_F32, x, M, K, q, scale, s, &ctx->launches);

@@ -121,7 +121,7 @@ def test_quantized_rows(ctx, rows, columns, dtype):
 
 
 PRODUCTS = [  # M, K, N
-    (1, 16, 1), (1, 16, 8), (2, 48, 3), (5, 112, 33), (8, 256, 72), (16, 4096, 64), (17, 128, 128), (33, 1040, 130), (128, 1024, 1000), (129, 272, 257),
+    (1, 16, 1), (1, 16, 8), (1, 4112, 33), (1, 20000, 10), (1, 1024, 9000), (2, 48, 3), (5, 112, 33), (8, 256, 72), (16, 4096, 64), (17, 128, 128), (33, 1040, 130), (128, 1024, 1000), (129, 272, 257),
     (200, 2000, 136), (256, 512, 512), (300, 144, 1500), (1000, 640, 768),
 ]
 
@@ -145,7 +145,7 @@ def test_int8_product(ctx, shape, out_dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=ids)
-@pytest.mark.parametrize("shape", [(1, 64, 64), (1, 37, 5), (3, 1000, 200), (8, 100, 1000), (24, 512, 96), (128, 1024, 1000), (500, 333, 640)], ids=str)
+@pytest.mark.parametrize("shape", [(1, 64, 64), (1, 37, 5), (1, 5000, 700), (1, 131072, 9), (2, 131071, 16), (3, 1000, 200), (8, 100, 1000), (24, 512, 96), (128, 1024, 1000), (500, 333, 640)], ids=str)
 def test_dense_int8(ctx, shape, dtype):
     M, K, N = shape
     x, bias = normal(4, (M, K), 1.0, dtype), normal(5, (N,), 0.1)
