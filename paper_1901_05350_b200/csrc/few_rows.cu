@@ -83,7 +83,7 @@ struct FewArgs {
 template <bool F32, bool X32, bool GATED, int T, bool VECTOR>
 __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant__ FewArgs a) {
     constexpr int M = GATED ? 2 : 1;
-    constexpr int U = T >= 8 || (GATED && T <= 2) ? 4 : 8;  // rows of weights in flight a thread and matrix
+    constexpr int U = T >= 8 ? 4 : 8;  // rows of weights in flight a thread and matrix
     extern __shared__ float xs[];      // [k][T] of this slice, a chunk at a time
     __shared__ float part[WARPS][M][T * 8][8];
     __shared__ float sums[M][T][COLUMNS];  // [slice][column of this CTA's share]: every CTA of the cluster writes its slice's part
@@ -262,11 +262,9 @@ cudaError_t launch_few(const FewArgs& a, bool vector, int64_t grid, cudaStream_t
 template <bool F32, bool X32, bool GATED>
 tfjsb_status few(tfjsb_ctx* ctx, const void* x, const void* w0, const void* w1, int gate, void* out, int64_t rows, int64_t N, int64_t K, cudaStream_t s) {
     FewArgs a = {x, w0, w1, out, N, (int)K, (int)rows, 0, 1, gate};
-    // As many slices as give each SM two blocks at most (three of the gated product of one or two rows, whose blocks are smaller) and each
-    // thread at least 4 rows of weights.
+    // As many slices as give each SM two blocks at most and each thread at least 4 rows of weights.
     const int64_t blocks = (N + COLUMNS - 1) / COLUMNS;
-    const int64_t most = (int64_t)(GATED && rows <= 2 ? 3 : 2) * ctx->sm_count;
-    while (a.splits < 8 && blocks * a.splits * 2 <= most && K / (a.splits * 2) >= 4 * K_LANES) a.splits *= 2;
+    while (a.splits < 8 && blocks * a.splits * 2 <= 2 * ctx->sm_count && K / (a.splits * 2) >= 4 * K_LANES) a.splits *= 2;
     a.k_per_slice = (int)((K + a.splits - 1) / a.splits);
     const bool vector = N % 8 == 0;  // pointers are 16-byte aligned
     const int64_t grid = blocks * a.splits;
@@ -293,7 +291,7 @@ struct FewInt8Args {
 
 // One row of x.  QUANTIZE: 0 x is 8-bit already, 1 bfloat16, 2 fp32.
 template <int QUANTIZE>
-__global__ void __launch_bounds__(THREADS) few_rows_int8_kernel(const __grid_constant__ FewInt8Args a) {
+__global__ void __launch_bounds__(THREADS, 4) few_rows_int8_kernel(const __grid_constant__ FewInt8Args a) {
     extern __shared__ __align__(16) int8_t q[];  // [pitch]
     __shared__ float largest[WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
