@@ -959,33 +959,36 @@ int64_t tiles_of(const Product& p, int cg, int block_n, int subs = 1) {
     return ((p.args.M + rows - 1) / rows) * ((p.args.N + columns - 1) / columns) * p.args.outputs;
 }
 
-// Estimated cycles, fitted to clocks read in the kernel (at about 1.9 GHz) and to whole products:
-//   - a k-block takes what its MMAs take (2 cycles a column and plane product) or what an SM can fetch (50 bytes a cycle), whichever
-//     is longer, but not less than issuing its MMAs takes (390); a pair with two parts fetches three tiles for two, a pair half of B, single CTAs everything;
-//   - the first k-block arrives 3400 cycles after the start (4200 in a pair), an epilogue warp takes 900 to 1950 cycles for a chunk;
-//   - with one part a tile the epilogue runs beside the next tile's K loop, with two it holds up the next tile for most of the time it takes;
-//   - slices cost two cluster barriers and a round trip for each share of the tile that a thread adds.
+// Estimated cycles, with constants fitted to 2200 measured times of products from 10 x 128 x 192 to 13248 x 256 x 2595 on every kernel shape (the shape
+// with the least estimate takes 1 % longer than the best in the mean, 13 % at most):
+//   - a k-block takes what its MMAs take, what an SM can fetch (48 to 63 bytes a cycle) or what issuing takes, whichever is longest; a pair
+//     with two parts fetches three tiles for two, a pair half of B, single CTAs everything;
+//   - the first k-block arrives, and the epilogue takes, so long; with one part a tile the epilogue runs beside the next tile's K
+//     loop, with two it holds up the next tile (by more than itself: tensor memory is read while both parts' MMAs write it);
+//   - slices cost two cluster barriers and a round trip for each share of the tile that a thread adds; clusters of more CTAs, each with an SM
+//     of its own in one group of SMs, also start later.
 double cost(const Product& p, const Shape& c, int sm_count) {
     const Args& a = p.args;
     const int kb = (a.K + (p.kind == KIND_BF16 ? 63 : 127)) / (p.kind == KIND_BF16 ? 64 : 128) * a.passes, own_kb = (kb + c.splits - 1) / c.splits;
     const double rows = a.M < ROWS ? a.M : ROWS;
     auto k_block = [&](int subs) {
-        const double fetch = p.planes * 128. * (rows * subs + c.block_n / c.cg) / 50, mma = 2.16 * c.block_n * subs * (p.planes == 3 ? 6 : 1);
-        const double longer = fetch > mma ? fetch : mma, issue = 390. * (p.planes == 3 ? 4 : 1);
+        const double rate = c.block_n == 256 ? (c.cg == 2 ? 48 : 50) : c.block_n == 64 ? 52.5 : 62.5;
+        const double fetch = p.planes * 128. * (rows * subs + c.block_n / c.cg) / rate, mma = 1.63 * c.block_n * subs * (p.planes == 3 ? 6 : 1);
+        const double longer = fetch > mma ? fetch : mma, issue = p.planes == 3 ? 975 : 450;
         return longer > issue ? longer : issue;
     };
-    const double main = own_kb * k_block(c.subs), first = c.cg == 2 ? 4200 : 3400;
+    const double main = own_kb * k_block(c.subs), first = c.cg == 2 ? 3600 : 2200;
     const int columns = p.epilogue == EPI_GATED ? c.block_n / 2 : c.block_n;
-    const double chunk = p.epilogue == EPI_STORE ? 900. / 32 : p.epilogue == EPI_SCALE ? 3000. / 32 : p.epilogue == EPI_GRAD ? 1800. / 16 : a.z ? 1400. / 16 : 1200. / 16;
-    const double epilogue = columns / 4 * chunk * (p.planes == 3 ? 2.5 : 1);
+    const double column = p.epilogue == EPI_STORE ? 25 : p.epilogue == EPI_SCALE ? 87 : p.epilogue == EPI_GRAD ? 101 : a.z ? 83 : 60;
+    const double epilogue = columns / 4 * column * (p.planes == 3 ? 5 : 1);
     const int64_t tiles = tiles_of(p, c.cg, c.block_n, c.subs), slots = sm_count / c.cg;
     if (c.splits > 1) {
         const int64_t shares = (int64_t)rows * (columns / 8), each = 32 * EPI_WARPS * c.splits;
-        return first + main + 4000 + (double)((shares + each - 1) / each) * 1500;
+        return first + main + (c.splits == 2 ? 2100 : c.splits == 4 ? 5700 : 9700) + (double)((shares + each - 1) / each) * 2950;
     }
     const int64_t rounds = tiles / slots, rest = tiles % slots;
     if (c.subs == 2) {
-        const double whole = main + 1.5 * epilogue;
+        const double whole = main + 3.7 * epilogue;
         return first + rounds * whole + (rest == 0 ? 0. : 2 * rest <= slots ? own_kb * k_block(1) + epilogue : whole) + epilogue;
     }
     const double step = main > epilogue ? main : epilogue;
@@ -1036,7 +1039,7 @@ Shape choose(const Product& p, int sm_count) {
             if (p.planes == 3 && bn != 128) continue;                         // two accumulators of 128 columns, two stages
             if (bn == 64 && (cg == 2 || p.epilogue == EPI_GATED)) continue;   // boxes are 64 columns wide
             const int64_t tiles = tiles_of(p, cg, bn);
-            for (int splits = 1; splits <= (cg == 1 && bn <= 128 ? 8 : 1); splits *= 2) {
+            for (int splits = 1; splits <= (cg == 1 ? 8 : 1); splits *= 2) {
                 // at least four k-blocks a slice, none without any, one wave
                 const int each = (kb + splits - 1) / splits;
                 if (splits > 1 && (each < 4 || each * (splits - 1) >= kb || tiles > resident_clusters(splits))) continue;

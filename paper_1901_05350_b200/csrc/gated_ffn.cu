@@ -19,19 +19,72 @@ namespace {
 
 // ---- copies into planes -----------------------------------------------------------------------------------
 // Matrices [rows, columns] as P planes of bfloat16 with rows of a multiple of 16 bytes: an fp32 matrix in three parts, a bfloat16 one whose
-// rows are not such a multiple as it is.  Several matrices in one launch, a block takes 2048 values of the concatenation of all rows of one.
+// rows are not such a multiple as it is.  Several matrices in one launch; a thread has eight values of a row at a time, LAYOUT_STEPS times.
+//
+// Rows begin anywhere, so a thread loads the aligned 16-byte pieces that its eight values lie in and moves them into place (eight loads of one
+// value each, which touch the same lines, took twice as long); the last pieces of a matrix, which may reach beyond its end, value by value.
 struct LayoutItem {
     const void* src;
     __nv_bfloat16* dst;
     int64_t rows, columns, pitch, plane;
     int64_t first_block;
 };
-constexpr int LAYOUT_MAX = 5, LAYOUT_PER_BLOCK = 2048;
+constexpr int LAYOUT_MAX = 5, LAYOUT_STEPS = 2, LAYOUT_PER_BLOCK = LAYOUT_STEPS * 2048;
 struct LayoutArgs {
     LayoutItem item[LAYOUT_MAX];
     int count = 0;
     int64_t blocks = 0;
 };
+
+__device__ __forceinline__ uint4 ld16(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+// Eight values of an item from `at` on (an index into the source), of which `left` are wanted; those beyond are anything.
+template <bool F32>
+__device__ __forceinline__ void source8(const LayoutItem& it, int64_t at, int left, float (&v)[8]) {
+    constexpr int SIZE = F32 ? 4 : 2, PIECES = F32 ? 3 : 2;
+    const char* p = static_cast<const char*>(it.src) + at * SIZE;
+    const int shift = (int)(reinterpret_cast<uintptr_t>(p) & 15u) / SIZE;  // values
+    const char* from = p - shift * SIZE;
+    const int64_t there = it.rows * it.columns * SIZE - (from - static_cast<const char*>(it.src));  // bytes from there to the end
+    if (there < 16 * PIECES) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[e] = 0.f;
+            if (e < left) {
+                if (F32) v[e] = load_global(reinterpret_cast<const float*>(p) + e);
+                else v[e] = __uint_as_float((uint32_t)load_global(reinterpret_cast<const unsigned short*>(p) + e) << 16);
+            }
+        }
+        return;
+    }
+    uint32_t w[4 * PIECES];
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) {
+        const uint4 q = ld16(from + 16 * j);
+        w[4 * j] = q.x; w[4 * j + 1] = q.y; w[4 * j + 2] = q.z; w[4 * j + 3] = q.w;
+    }
+    const int words = F32 ? shift : shift >> 1;
+    if (words & 1) {
+#pragma unroll
+        for (int i = 0; i + 1 < 4 * PIECES; ++i) w[i] = w[i + 1];
+    }
+    if (words & 2) {
+#pragma unroll
+        for (int i = 0; i + 2 < 4 * PIECES; ++i) w[i] = w[i + 2];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (F32) {
+            v[e] = __uint_as_float(w[e]);
+        } else {
+            const uint32_t pair = (shift & 1) ? __funnelshift_r(w[e / 2], w[e / 2 + 1], 16) : w[e / 2];
+            v[e] = __uint_as_float(e % 2 ? pair & 0xffff0000u : pair << 16);
+        }
+    }
+}
 
 template <bool F32>
 __global__ void __launch_bounds__(256) layout_kernel(const __grid_constant__ LayoutArgs args) {
@@ -40,21 +93,24 @@ __global__ void __launch_bounds__(256) layout_kernel(const __grid_constant__ Lay
     int k = 0;
     while (k + 1 < args.count && (int64_t)blockIdx.x >= args.item[k + 1].first_block) ++k;
     const LayoutItem& it = args.item[k];
-    // eight values of one row a thread; the pitch is a multiple of eight
-    const int64_t at = (((int64_t)blockIdx.x - it.first_block) * 256 + threadIdx.x) * 8;
-    const int64_t row = at / it.pitch;
-    const int col = (int)(at - row * it.pitch);
-    if (row >= it.rows) return;
-    const int left = (int)(it.columns - col);
-    float v[8];
-    if (F32) {
-        load_f32(static_cast<const float*>(it.src) + row * it.columns + col, v, left);
-        store_planes<3>(it.dst + row * it.pitch + col, it.plane, v, 8);
-    } else {
-        const unsigned short* src = static_cast<const unsigned short*>(it.src) + row * it.columns + col;
+    float v[LAYOUT_STEPS][8];
+    int64_t row[LAYOUT_STEPS];
+    int col[LAYOUT_STEPS];
+    const uint32_t per_row = (uint32_t)(it.pitch >> 3);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? __uint_as_float((uint32_t)load_global(src + i) << 16) : 0.f;
-        store_planes<1>(it.dst + row * it.pitch + col, it.plane, v, 8);
+    for (int s = 0; s < LAYOUT_STEPS; ++s) {
+        const int64_t eights = ((int64_t)blockIdx.x - it.first_block) * (LAYOUT_PER_BLOCK / 8) + s * 256 + threadIdx.x;
+        row[s] = eights < (1LL << 31) ? (int64_t)((uint32_t)eights / per_row) : eights / per_row;
+        col[s] = (int)(eights - row[s] * per_row) * 8;
+        if (row[s] < it.rows) source8<F32>(it, row[s] * it.columns + col[s], (int)(it.columns - col[s]), v[s]);
+    }
+#pragma unroll
+    for (int s = 0; s < LAYOUT_STEPS; ++s) {
+        if (row[s] >= it.rows) continue;
+        const int left = (int)(it.columns - col[s]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[s][e] = e < left ? v[s][e] : 0.f;
+        store_planes<F32 ? 3 : 1>(it.dst + row[s] * it.pitch + col[s], it.plane, v[s], 8);
     }
 }
 
