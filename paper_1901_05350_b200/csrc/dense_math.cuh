@@ -18,7 +18,11 @@ namespace dense {
 // exponential's 2^-21 is nothing.
 template <bool EXACT>
 __device__ __forceinline__ float logistic(float v) {
-    if (EXACT) return 1.f / (1.f + expf(-v));
+    if (EXACT) {
+        float r;
+        asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + expf(-v)));  // within an ulp; 0 of an infinity
+        return r;
+    }
     return __fdividef(1.f, 1.f + __expf(-v));  // e^-v = inf: 0
 }
 
@@ -144,49 +148,57 @@ __device__ __forceinline__ void load_f32(const float* p, float (&v)[W], int left
         }
     }
 }
+// Pairs of bfloat16.
 template <int W>
-__device__ __forceinline__ void store_bf16(__nv_bfloat16* p, const float (&v)[W], int left) {
+__device__ __forceinline__ void store_pairs(__nv_bfloat16* p, const uint32_t (&w)[W / 2], int left) {
     const bool sector = aligned(p, 32), quad = aligned(p, 16);
     constexpr int G = W < 16 ? 8 : 16;
 #pragma unroll
     for (int j = 0; j < W; j += G) {
-        uint32_t w[G / 2];
-#pragma unroll
-        for (int i = 0; i < G / 2; ++i) w[i] = pack_bf16(v[j + 2 * i], v[j + 2 * i + 1]);
         if (G == 16 && j + G <= left && sector) {
-            st32(p + j, w);
+            st32(p + j, &w[j / 2]);
         } else if (j + G <= left && quad) {
-            st16(p + j, w);
-            if (G == 16) st16(p + j + 8, w + G / 4);
+            st16(p + j, &w[j / 2]);
+            if (G == 16) st16(p + j + 8, &w[j / 2 + G / 4]);
         } else {
 #pragma unroll
             for (int i = 0; i < G; ++i)
-                if (j + i < left) p[j + i] = __ushort_as_bfloat16((unsigned short)(w[i / 2] >> (i % 2 * 16)));
+                if (j + i < left) p[j + i] = __ushort_as_bfloat16((unsigned short)(w[(j + i) / 2] >> (i % 2 * 16)));
         }
     }
 }
-
-// v as P bfloat16 planes: itself, rounded to nearest (P = 1), or three whose sum is v, each the rest of the one before
-// rounded to nearest.  A first plane that rounds to infinity takes the largest bfloat16 instead, so that the sum is v; of an infinity or
-// a NaN the other planes are zero.
-__device__ __forceinline__ void split3(float v, float& p0, float& p1, float& p2) {
-    p0 = __bfloat162float(__float2bfloat16_rn(v));
-    if (isinf(p0)) p0 = isinf(v) ? v : copysignf(__uint_as_float(0x7f7f0000u), v);
-    const float r = isfinite(p0) ? v - p0 : 0.f;
-    p1 = __bfloat162float(__float2bfloat16_rn(r));
-    p2 = __bfloat162float(__float2bfloat16_rn(r - p1));
+template <int W>
+__device__ __forceinline__ void store_bf16(__nv_bfloat16* p, const float (&v)[W], int left) {
+    uint32_t w[W / 2];
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    store_pairs<W>(p, w, left);
 }
+
+// Values as P bfloat16 planes: themselves, rounded to nearest (P = 1), or three whose sum they are, each the rest of the one before
+// rounded to nearest.  Of a value beyond the largest bfloat16 the first plane is that, so that the sum holds; of an infinity or a NaN the planes'
+// sum is a NaN.
 template <int P, int W>
 __device__ __forceinline__ void store_planes(__nv_bfloat16* p, int64_t plane, const float (&v)[W], int left) {
     if constexpr (P == 1) {
         store_bf16(p, v, left);
     } else {
-        float p0[W], p1[W], p2[W];
+        const float most = __uint_as_float(0x7f7f0000u);
+        uint32_t w[W / 2];
+        float r[W];
 #pragma unroll
-        for (int i = 0; i < W; ++i) split3(v[i], p0[i], p1[i], p2[i]);
-        store_bf16(p, p0, left);
-        store_bf16(p + plane, p1, left);
-        store_bf16(p + 2 * plane, p2, left);
+        for (int i = 0; i < W / 2; ++i) w[i] = pack_bf16(fminf(fmaxf(v[2 * i], -most), most), fminf(fmaxf(v[2 * i + 1], -most), most));
+#pragma unroll
+        for (int i = 0; i < W; ++i) r[i] = v[i] - __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        store_pairs<W>(p, w, left);
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) w[i] = pack_bf16(r[2 * i], r[2 * i + 1]);
+#pragma unroll
+        for (int i = 0; i < W; ++i) r[i] -= __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        store_pairs<W>(p + plane, w, left);
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) w[i] = pack_bf16(r[2 * i], r[2 * i + 1]);
+        store_pairs<W>(p + 2 * plane, w, left);
     }
 }
 

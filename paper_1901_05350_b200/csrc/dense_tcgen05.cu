@@ -183,6 +183,12 @@ __device__ __forceinline__ Item item_at(const Args& a, int item) {
     return it;
 }
 
+// Eight of W values.
+template <int W>
+__device__ __forceinline__ float (&eight(float (&v)[W], int j))[8] {
+    return reinterpret_cast<float(&)[8]>(v[j]);
+}
+
 // ---- what becomes of W sums of a row -------------------------------------------------------------------
 // `first` and, for EPI_GATED, `second` are the sums (g and u) of columns col .. col + W - 1 of row `row`; W is 8, 16 or 32.
 template <int P, int W>
@@ -235,15 +241,23 @@ __device__ __forceinline__ void finish(const Args& a, int which, int64_t row, in
 #pragma unroll
         for (int i = 0; i < W; ++i) { g[i] = __uint_as_float(first[i]); u[i] = __uint_as_float(second[i]); }
         if (a.z) {
-            store_f32(z_at(a, row, col, 0), g, W);
-            store_f32(z_at(a, row, col, 1), u, W);
+#pragma unroll
+            for (int j = 0; j < W; j += 8) {
+                if (j >= left) break;
+                store_f32(z_at(a, row, col + j, 0), eight(g, j), 8);
+                store_f32(z_at(a, row, col + j, 1), eight(u, j), 8);
+            }
         }
         gated<P == 3>(a.gate, g, u, v);
         store_planes<P>(static_cast<__nv_bfloat16*>(a.out[0]) + row * a.out_pitch + col, a.out_plane, v, left);
     } else {
         float g[W], u[W];
-        load_f32(z_at(a, row, col, 0), g, W);
-        load_f32(z_at(a, row, col, 1), u, W);
+#pragma unroll
+        for (int j = 0; j < W; j += 8) {
+            if (j >= left) break;
+            load_f32(z_at(a, row, col + j, 0), eight(g, j), 8);
+            load_f32(z_at(a, row, col + j, 1), eight(u, j), 8);
+        }
         finish_gradient<P, W>(a, row, col, first, g, u);
     }
 }
@@ -780,23 +794,18 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
             if constexpr (P == 3) {
                 if (ok && args.splits == 1) {
                     const int64_t row = m0 + quad * 32 + lane;
-                    // Eight columns at a time in a rolled loop; the sums move up in their registers instead of being indexed.
+                    // Sixteen columns at a time, 32 bytes of each plane of a row: what stores cost goes by the rows that they touch.
+                    uint32_t w0[16], w1[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) { w0[i] = __float_as_uint(sum[0][i]); w1[i] = __float_as_uint(sum[1][i]); }
+                    if (EPI == EPI_GATED) {
+                        finish<P, EPI, 16>(args, which, row, n0 + part * 16, w0, w1);
+                    } else {
 #pragma unroll 1
-                    for (int c = 0; c < 16; c += 8) {
-                        uint32_t w0[8], w1[8];
+                        for (int j = 0; j < 2; ++j) {
+                            finish<P, EPI, 16>(args, which, row, n0 + (part + PARTS * j) * 16, w0, w0);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) { w0[i] = __float_as_uint(sum[0][i]); w1[i] = __float_as_uint(sum[1][i]); }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) { sum[0][i] = sum[0][i + 8]; sum[1][i] = sum[1][i + 8]; }
-                        if (EPI == EPI_GATED) {
-                            finish<P, EPI, 8>(args, which, row, n0 + part * 16 + c, w0, w1);
-                        } else {
-#pragma unroll 1
-                            for (int j = 0; j < 2; ++j) {
-                                finish<P, EPI, 8>(args, which, row, n0 + (part + PARTS * j) * 16 + c, w0, w0);
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) w0[i] = w1[i];
-                            }
+                            for (int i = 0; i < 16; ++i) w0[i] = w1[i];
                         }
                     }
                 }
