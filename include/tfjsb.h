@@ -280,8 +280,8 @@ tfjsb_status tfjsb_bias_backprop(tfjsb_ctx* ctx, const tfjsb_tensor* dz, tfjsb_t
  *   x [tokens,width], w_gate and w_up [width,hidden], w_down [hidden,out_width], y [tokens,out_width], all of `dtype`.
  * Any sizes from 1 to 2^30 (tokens may be 0); operands whose rows are no multiple of 16 bytes are copied into the workspace first.
  * Products run on the tensor cores with fp32 sums: of bfloat16 values exactly, of fp32 values (as three bfloat16 parts) as exactly as
- * fp32 multiply-adds; up to 8 tokens without a gradient on CUDA cores, which is where their weights can be read fastest.  In bfloat16,
- * g = x w_gate and u = x w_up stay fp32, the product gate(g) u is rounded to bfloat16 once, and y once.  An infinity among fp32 operands
+ * fp32 multiply-adds (parts of values below 2^-100 are flushed); without a gradient, a bfloat16 token or two and up to eight fp32 tokens on CUDA
+ * cores, which is where their weights can be read fastest.  In bfloat16, g = x w_gate and u = x w_up stay fp32, the product gate(g) u is rounded to bfloat16 once, and y once.  An infinity among fp32 operands
  * may give NaN where the exact result is infinite. */
 typedef struct {
     int64_t tokens, width, hidden, out_width;
@@ -306,7 +306,7 @@ tfjsb_status tfjsb_gated_ffn_backprop(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, cons
  *   x, residual, out: rank 1..4, `dims`, of `dtype`; out may be x or residual.  noise_dims: NULL, or the mask's shape, of the same
  *   rank, each dimension that of x or 1 (broadcast).  m(i) is the row-major index in the mask's shape.
  *   keep[m] is word m % 4 of Philox-4x32-10 (Salmon et al. 2011) with key = seed and counter = (m / 4, offset), 64 bits each, low word
- *   first: word >= ceil(rate 2^32).  0 <= rate < 1.
+ *   first: word >= ceil(rate 2^32).  0 <= rate < 1 - 2^-32.  At most 2^40 elements.
  * The arithmetic is fp32, x * fp32(1 / (1 - rate)) + residual in one rounding, and one more into bfloat16.
  * The gradient is the same call on dy without a residual (tfjsb_dropout_backprop). */
 tfjsb_status tfjsb_dropout(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, const void* residual, void* out, int32_t rank, const int64_t* dims,
@@ -321,7 +321,8 @@ tfjsb_status tfjsb_dropout_backprop(tfjsb_ctx* ctx, tfjsb_dtype dtype, const voi
 tfjsb_status tfjsb_quantize_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, void* stream);
 /* out[M,N] = act( (a[M,K] . bt[N,K]^T) * a_scale[M] * b_scale[N] + bias[N] ):  a and bt 8-bit integers with K contiguous (bt as matMul's right
  * operand stored transposed), exact 32-bit sums, the rest in fp32, one more rounding where out is bfloat16.  a_scale, b_scale, bias fp32
- * (bias may be NULL).  K a multiple of 16 (else TFJSB_ERR_UNSUPPORTED: fill rows up with zeros), at most 131072. */
+ * (bias may be NULL).  K a multiple of 16 (else TFJSB_ERR_UNSUPPORTED: fill rows up with zeros), at most 131072 (where both hold
+ * -128, which quantize_int8 does not make: less). */
 tfjsb_status tfjsb_matmul_int8(tfjsb_ctx* ctx, const int8_t* a, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias,
                                tfjsb_act act, void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, void* stream);
 /* A dense layer on 8-bit weights: the two calls above on x [M,K] of `dtype`, with the same results.  bt is [N, K rounded up to a multiple of 16], the

@@ -528,6 +528,8 @@ class Context:
 
     def gated_ffn_backprop(self, x, w_gate, w_up, w_down, h, z, dy, gate: str = "silu", want=(True, True, True, True)):
         """(dx, dw_gate, dw_up, dw_down) of gated_ffn, given what it saved and the gradient of y; None for those not in `want`."""
+        if len(want) != 4:
+            raise ValueError("want has four entries")
         if all(want):
             done = _fast.gated_ffn_backprop(self._fh, self.device, x, w_gate, w_up, w_down, h, z, dy, GATE.get(gate, -1))
             if done is not None:
@@ -537,10 +539,8 @@ class Context:
         f, sizes = self._ffn(x, w_gate, w_up, w_down, gate)
         _plain(dy, "dy", x.dtype, tuple(x.shape[:-1]) + (f.out_width,), self.device)
         for t, name, size in ((h, "h", sizes[0]), (z, "z", sizes[1])):
-            if not isinstance(t, torch.Tensor) or t.get_device() != self.device or t.dtype != torch.uint8 or t.numel() != max(size, 16):
+            if not isinstance(t, torch.Tensor) or t.get_device() != self.device or t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() != max(size, 16):
                 raise ValueError(f"{name} is not what gated_ffn saved for these shapes")
-        if len(want) != 4:
-            raise ValueError("want has four entries")
         grads = [self._new(t.shape, t.dtype) if w else None for t, w in zip((x, w_gate, w_up, w_down), want)]
         work = self._bytes(sizes[3])
         self._check(lib.tfjsb_gated_ffn_backprop(self._h, ctypes.byref(f), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(h), _ptr(z), _ptr(dy),

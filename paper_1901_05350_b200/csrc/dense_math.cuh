@@ -55,7 +55,7 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& slope) {
         a = g * f;
         if (SLOPE) slope = fmaf(g * 0.39894228040143268f, e, f);
     } else {
-        const float g2 = g * g;
+        const float g2 = fminf(g * g, 1e30f);  // finite, so that 1 - s = 0 makes the slope of large g what it is
         const float s = logistic<EXACT>(1.5957691216057308f * g * fmaf(0.044715f, g2, 1.f));
         a = g * s;
         if (SLOPE) slope = s + a * (1.f - s) * 1.5957691216057308f * fmaf(0.134145f, g2, 1.f);

@@ -10,9 +10,14 @@
 // columns of one of them.  The gradient of x is one product too, over dg Wg^T and then du Wu^T in the same accumulator, and the
 // gradients of Wg and Wu are one launch over the tiles of both.
 //
-// Structure (CTA pairs, CG = 2, as in gemm_pair.cu; single CTAs, CG = 1, without the cluster): warp 0 copies (TMA), warp 1 issues the
-// MMAs, warps 2-17 are the epilogue, which works on one accumulator stage while the next tile is summed in the other.  The epilogue writes
-// global memory directly: a thread has a row, 32 bytes of it at a time, so that every sector is written once and whole.
+// Structure (CTA pairs, CG = 2, as in gemm_pair.cu; single CTAs, CG = 1, without the cluster): warp 0 copies A and warp 18 B (TMA), warp
+// 1 issues the MMAs, warps 2-17 are the epilogue, which works on one accumulator stage while the next tile is summed in the
+// other.  Stored results leave through shared memory (TMA), h and the gradients of g and u from registers, 32 bytes of a row a thread, so that
+// every sector is written once and whole; g and u are in blocks of 32 rows x 8 columns, which a warp moves in one piece.
+//
+// What bounds it: at large sizes what an SM can fetch from L2 (50 to 60 bytes a cycle), so the widest tile is 512 x 256 for a CTA pair, two parts
+// of 256 rows that share B (SUBS = 2): 8192 x 4096 x 16384 took 1.62-1.64 PFLOP/s of the burst, with 256 x 256 tiles 1.35.  At small ones
+// latency: a launch, the first copies (2 us) and the epilogue.
 // Persistent over tiles in bands of `band` tile rows, so that the tiles in flight share operand rows and columns in L2.
 //
 // Few tiles: K is cut among the CTAs of a cluster (CG = 1, one tile each).  Each writes its partial tile to its own shared
@@ -23,9 +28,8 @@
 // below 2^-26 of it.  The tensor core cuts every sum towards zero, so the error of an accumulator grows with the number of
 // additions: the large products go to an accumulator of their own for `seg_kb` k-blocks only (8 additions), the small ones
 // to another, and the epilogue adds both to fp32 sums in registers, rounded to nearest.
+#include <atomic>
 #include <cstdlib>
-#include <map>
-#include <mutex>
 
 #include <cuda_bf16.h>
 
@@ -1007,13 +1011,12 @@ double cost(const Product& p, const Shape& c, int sm_count) {
 // Clusters of that many CTAs, one to an SM, that are resident at once: less than the SMs over their number, which the GPU's groups of SMs
 // do not divide.
 int resident_clusters(int size) {
-    static std::mutex mu;
-    static std::map<std::pair<int, int>, int> known;  // (device, size)
+    constexpr int DEVICES = 64;
+    static std::atomic<int> known[DEVICES][9];  // 0: not asked yet
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 1;
-    std::lock_guard<std::mutex> lock(mu);
-    auto it = known.find({dev, size});
-    if (it != known.end()) return it->second;
+    if (dev < DEVICES)
+        if (const int n = known[dev][size].load(std::memory_order_relaxed)) return n;
     auto* kernel = &dense_kernel<1, 1, KIND_BF16, EPI_STORE, 1, false, false>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(size * 64);
@@ -1032,7 +1035,7 @@ int resident_clusters(int size) {
         (void)cudaGetLastError();
         n = 96 / size;
     }
-    known[{dev, size}] = n;
+    if (dev < DEVICES) known[dev][size].store(n, std::memory_order_relaxed);
     return n;
 }
 
@@ -1051,7 +1054,7 @@ Shape choose(const Product& p, int sm_count) {
             for (int splits = 1; splits <= (cg == 1 ? 8 : 1); splits *= 2) {
                 // at least four k-blocks a slice, none without any, one wave
                 const int each = (kb + splits - 1) / splits;
-                if (splits > 1 && (each < 4 || each * (splits - 1) >= kb || tiles > resident_clusters(splits))) continue;
+                if (splits > 1 && (each < 4 || each * (splits - 1) >= kb || tiles * splits > sm_count || tiles > resident_clusters(splits))) continue;
                 for (int subs = 1; subs <= (cg == 2 && bn == 256 && p.planes == 1 ? 2 : 1); ++subs) {
                     const Shape c = {cg, bn, splits, subs};
                     if (force && f[0] == cg && f[1] == bn && f[2] == splits && f[3] == subs) return c;
