@@ -571,7 +571,10 @@ def test_projections_that_are_enormous(ctx, gate, dtype):
     x, wu = x * 1e20, wu * 1e-20
     y, h, z = ctx.gated_ffn(x, wg, wu, wd, gate=gate, save=True)
     grads = ctx.gated_ffn_backprop(x, wg, wu, wd, h, z, dy, gate=gate)
-    for got, want in zip((y, *grads), (ref.gated_ffn(x, wg, wu, wd, gate), *ref.gated_ffn_gradients(x, wg, wu, wd, dy, gate))):
+    for i, (got, want) in enumerate(zip((y, *grads), (ref.gated_ffn(x, wg, wu, wd, gate), *ref.gated_ffn_gradients(x, wg, wu, wd, dy, gate)))):
+        if i == 3:  # dw_up = x^T du, du = dh gate(g): terms of 10^20 times 10^20, which neither type has numbers for
+            assert (want.abs() > 3.4e38).any()
+            continue
         assert torch.isfinite(got).all()
         assert ((got.double() - want).norm() / want.norm()).item() <= (2.0 ** -8 if dtype == torch.bfloat16 else 2e-6)
 
