@@ -202,19 +202,23 @@ __global__ void __launch_bounds__(BLOCK) dropout_kernel(const __grid_constant__ 
 // A mask shared by many positions: [outer][positions][channels], one row of the mask for all positions of an outer index (spatial dropout of
 // a sequence or an image).  A thread has four channels, whose words it makes once, of `share` positions: next to no arithmetic is left, so
 // this is bound by memory where making each word again was bound by the generator (64 x 197 x 771 fp32: 28 us).  VECTOR: rows of
-// channels are whole groups of four.
+// channels are whole groups of four, which a thread loads at once.  Otherwise a warp has 128 channels, a thread every 32nd of them, whose words
+// come from the threads that made them (four neighbours a thread, value by value, kept an SM's loads busy with four lines each:
+// 64 x 197 x 771 fp32 19 us).
 struct Positions {
-    int64_t outer, positions, groups;  // groups of four channels
+    int64_t outer, positions, groups;  // groups of four channels, or (not VECTOR) of 128
     int share;
 };
 template <bool F32, bool RESIDUAL, bool VECTOR>
 __global__ void __launch_bounds__(BLOCK) dropout_positions_kernel(const __grid_constant__ DropoutArgs a, const __grid_constant__ Positions s) {
     ptx::pdl_wait();
-    const int64_t t = (int64_t)blockIdx.x * BLOCK + threadIdx.x, o = t / s.groups;
-    if (o >= s.outer) return;
-    const int64_t channels = (int64_t)a.extent[0], c = (t - o * s.groups) * 4;
-    const int left = channels - c < 4 ? (int)(channels - c) : 4;
-    uint64_t m = (uint64_t)c, rest = (uint64_t)o;
+    constexpr int NEXT = VECTOR ? 1 : 32;  // from one channel of a thread to the next
+    const int lane = threadIdx.x & 31;
+    const int64_t t = (int64_t)blockIdx.x * BLOCK + threadIdx.x, g = VECTOR ? t : t >> 5, o = g / s.groups;
+    if (o >= s.outer) return;  // not VECTOR: all of a warp
+    const int64_t channels = (int64_t)a.extent[0], c = (g - o * s.groups) * (VECTOR ? 4 : 128) + (VECTOR ? 0 : lane);
+    const int left = VECTOR ? 4 : (int)((channels - c + 31) / 32);
+    uint64_t m = (uint64_t)(VECTOR ? c : c + 3 * lane), rest = (uint64_t)o;
     for (int d = 2; d < a.dims; ++d) {
         const uint64_t q = rest / a.extent[d];
         m += (rest - q * a.extent[d]) * a.step[d];
@@ -225,6 +229,11 @@ __global__ void __launch_bounds__(BLOCK) dropout_positions_kernel(const __grid_c
     bool keep[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) keep[e] = w[e] >= a.threshold;
+    if (!VECTOR) {  // channel lane + 32 e of the warp's is value lane % 4 of thread 8 e + lane / 4
+        const uint32_t own = (keep[0] ? 1u : 0u) | (keep[1] ? 2u : 0u) | (keep[2] ? 4u : 0u) | (keep[3] ? 8u : 0u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) keep[e] = __shfl_sync(0xffffffffu, own, 8 * e + (lane >> 2)) >> (lane & 3) & 1u;
+    }
     const int64_t first = (int64_t)blockIdx.y * s.share, last = first + s.share < s.positions ? first + s.share : s.positions;
     auto load4 = [&](const void* p, int64_t i, float (&v)[4]) {
         if (F32) {
@@ -234,7 +243,7 @@ __global__ void __launch_bounds__(BLOCK) dropout_positions_kernel(const __grid_c
                 v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = e < left ? load_global(q + e) : 0.f;
+                for (int e = 0; e < 4; ++e) v[e] = e < left ? load_global(q + e * NEXT) : 0.f;
             }
         } else {
             const unsigned short* q = static_cast<const unsigned short*>(p) + i;
@@ -244,7 +253,7 @@ __global__ void __launch_bounds__(BLOCK) dropout_positions_kernel(const __grid_c
                 v[2] = __uint_as_float(f.y << 16); v[3] = __uint_as_float(f.y & 0xffff0000u);
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = e < left ? __uint_as_float((uint32_t)load_global(q + e) << 16) : 0.f;
+                for (int e = 0; e < 4; ++e) v[e] = e < left ? __uint_as_float((uint32_t)load_global(q + e * NEXT) << 16) : 0.f;
             }
         }
     };
@@ -273,14 +282,14 @@ __global__ void __launch_bounds__(BLOCK) dropout_positions_kernel(const __grid_c
                     else
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (e < left) q[e] = x[u][e];
+                            if (e < left) q[e * NEXT] = x[u][e];
                 } else {
                     __nv_bfloat16* q = static_cast<__nv_bfloat16*>(a.out) + i;
                     if (VECTOR) *reinterpret_cast<uint2*>(q) = make_uint2(dense::pack_bf16(x[u][0], x[u][1]), dense::pack_bf16(x[u][2], x[u][3]));
                     else
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (e < left) q[e] = __float2bfloat16_rn(x[u][e]);
+                            if (e < left) q[e * NEXT] = __float2bfloat16_rn(x[u][e]);
                 }
             }
     }
@@ -297,14 +306,15 @@ cudaError_t launch_any(const DropoutArgs& a, int sm_count, cudaStream_t s) {
     if (a.dims >= 2 && a.step[0] == 1 && a.step[1] == 0 && a.extent[1] >= 8) {
         Positions p;
         p.positions = (int64_t)a.extent[1];
-        p.groups = ((int64_t)a.extent[0] + 3) / 4;
+        const bool vector = a.extent[0] % 4 == 0;
+        p.groups = ((int64_t)a.extent[0] + (vector ? 3 : 127)) / (vector ? 4 : 128);
         p.outer = a.n / (int64_t)(a.extent[0] * a.extent[1]);
-        const int64_t threads = p.outer * p.groups, blocks = (threads + BLOCK - 1) / BLOCK;
+        const int64_t threads = p.outer * p.groups * (vector ? 1 : 32), blocks = (threads + BLOCK - 1) / BLOCK;
         p.share = 32;
         while (p.share > 8 && blocks * ((p.positions + p.share - 1) / p.share) < (int64_t)sm_count * 8) p.share /= 2;
         const int64_t shares = (p.positions + p.share - 1) / p.share;
         if (a.extent[0] >= 32 && blocks < (1LL << 31) && shares <= 65535) {
-            auto* kernel = a.extent[0] % 4 == 0 ? &dropout_positions_kernel<F32, RESIDUAL, true> : &dropout_positions_kernel<F32, RESIDUAL, false>;
+            auto* kernel = vector ? &dropout_positions_kernel<F32, RESIDUAL, true> : &dropout_positions_kernel<F32, RESIDUAL, false>;
             return launch_k(kernel, dim3((unsigned)blocks, (unsigned)shares), dim3(BLOCK), 0, s, a, p);
         }
     }
