@@ -33,6 +33,7 @@ struct Args {
     int n_tiles = 0, m_tiles = 0, outputs = 1, num_tiles = 0, whole_tiles = 0, band = 8;
     int passes = 1, num_kb = 0, kb_per_split = 0, seg_kb = 0;
     int splits = 1;
+    int parts_apart = 0;                   // the slices' sums have shared memory of their own
     int a_rows = 0;
     void* out[2] = {nullptr, nullptr};
     int64_t out_pitch = 0, out_plane = 0;  // elements

@@ -99,37 +99,41 @@ __device__ __forceinline__ void load3(uint32_t dst, const CUtensorMap* map, uint
 __device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-__device__ __forceinline__ uint4 lds4_cluster(uint32_t addr) {
+__device__ __forceinline__ void sts16_cluster(uint32_t at, const uint32_t* v) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+
+__device__ __forceinline__ uint4 lds4u(uint32_t at) {
     uint4 v;
-    asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
 
 __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[16]) { tc_ld_cols(at, r); }
 __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[8]) { tc_ld_cols(at, r); }
 
-// The sum of eight columns' parts, from the shared memory of the cluster's CTAs: those of four slices on their way at once (a round trip
-// takes about half a microsecond), added in the order of the slices.
+// Where the slices of a tile (few tiles, K cut among the CTAs of a cluster) put their sums: the tile's columns are shared out among the CTAs, and
+// each has room for its share of every slice's rows, in rows of `pitch` values; a gated tile's for g and then for u.
+struct Share {
+    int columns, pitch, rows, planes;  // of a CTA's share
+    __host__ __device__ Share(const Args& a, bool gated) {
+        planes = gated ? 2 : 1;
+        columns = a.block_n / planes / a.splits;
+        pitch = columns + 4;  // consecutive rows start in other banks
+        rows = a.M < ROWS ? a.M : ROWS;
+    }
+    __host__ __device__ int at(int slice, int plane, int row) const { return ((slice * planes + plane) * rows + row) * pitch; }
+    __host__ __device__ int bytes(int slices) const { return at(slices, 0, 0) * 4; }
+};
+// The sum of eight columns, added in the order of the slices, `step` bytes apart.
 template <int KIND>
-__device__ __forceinline__ void pull_parts(uint32_t at, int splits, uint32_t (&sum)[8]) {
+__device__ __forceinline__ void sum_parts(uint32_t at, uint32_t step, int splits, uint32_t (&sum)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0u;
-#pragma unroll 1
-    for (int r = 0; r < splits; r += 4) {
-        uint4 x[4][2];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (r + j < splits) {
-                const uint32_t from = map_to_cta(at, (uint32_t)(r + j));
-                x[j][0] = lds4_cluster(from);
-                x[j][1] = lds4_cluster(from + 16u);
-            }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (r + j < splits) {
-                add_part<KIND>(sum, 0, x[j][0]);
-                add_part<KIND>(sum, 4, x[j][1]);
-            }
+#pragma unroll 4
+    for (int r = 0; r < splits; ++r) {
+        add_part<KIND>(sum, 0, lds4u(at + (uint32_t)r * step));
+        add_part<KIND>(sum, 4, lds4u(at + (uint32_t)r * step + 16u));
     }
 }
 
@@ -317,6 +321,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
     constexpr int BK = KIND == KIND_BF16 ? 64 : 128;
     const uint32_t acc_cols = (uint32_t)block_n * (P == 3 ? 2u : 1u);  // of an accumulator stage: large | small
     const uint32_t stage_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t parts_base = stage_base + (args.parts_apart ? (uint32_t)stages * stage_bytes : 0u);  // see Share
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) {
@@ -352,6 +357,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
         cluster_wait();
     }
     tc_fence_after();
+    if (CG == 1 && args.splits > 1 && args.parts_apart) cluster_arrive();  // "has begun": others may put their sums here
     const uint32_t tmem_base = tmem_base_slot;
     // Each role waits for the kernel before on its own: the producers only where that kernel may still write what they read (args.early_*), the
     // epilogue always, before it reads or writes anything, and the next kernel is let go after that wait.  So when a kernel of a chain
@@ -596,7 +602,6 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
         const int chunk = EPI == EPI_STORE || (EPI == EPI_SCALE && args.out_bf16) ? 32 : 16;  // columns
         const int n_chunks = block_n / chunk / (EPI == EPI_GATED ? 2 : 1);  // chunks, or pairs of them
         const int segments = P == 3 ? (kb_end - kb_begin + args.seg_kb - 1) / args.seg_kb : 1;
-        const uint32_t pitch = (uint32_t)(block_n + 4) * 4u;  // of a partial tile's row: consecutive rows start 4 banks apart
         const int ew = warp - 2;
         const uint32_t slab = stage_base + (uint32_t)stages * stage_bytes + (uint32_t)(ew * SLAB);
         uint32_t z_phase = 0;
@@ -836,10 +841,12 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
             }
             if constexpr (CG == 1) {
                 if (args.splits > 1) {
-                    // every MMA of this CTA has finished, so the stages' shared memory is free for the partial tile
-                    const uint32_t row_at = stage_base + (uint32_t)(quad * 32 + lane) * pitch;
+                    // Every CTA's MMAs have finished (or it has room of its own for the sums): each gets its columns of this slice's.
+                    if (!args.parts_apart) cluster_arrive();
+                    cluster_wait();
                     if (ok && m0 + quad * 32 < args.M) {
-                        // 16 columns at a time
+                        const Share share(args, EPI == EPI_GATED);
+                        const int columns = EPI == EPI_GATED ? block_n >> 1 : block_n;
 #pragma unroll 1
                         for (int j = 0; part + PARTS * j < block_n / 16; ++j) {
                             const int ch = part + PARTS * j;
@@ -852,7 +859,15 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                                 tc_ld_wait();
                             }
 #pragma unroll
-                            for (int i = 0; i < 16; i += 4) sts16(row_at + (uint32_t)(ch * 16 + i) * 4u, v[i], v[i + 1], v[i + 2], v[i + 3]);
+                            for (int i = 0; i < 16; i += 8) {
+                                const int plane = EPI == EPI_GATED && ch * 16 >= columns ? 1 : 0, col = ch * 16 + i - plane * columns;
+                                const int owner = col / share.columns;
+                                const uint32_t to = map_to_cta(parts_base + (uint32_t)(share.at((int)slice, plane, quad * 32 + lane) + col - owner * share.columns) * 4u,
+                                                               (uint32_t)owner);
+                                if (m0 + quad * 32 + lane >= args.M) continue;
+                                sts16_cluster(to, &v[i]);
+                                sts16_cluster(to + 16u, &v[i + 4]);
+                            }
                         }
                     }
                 }
@@ -865,8 +880,12 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
 
     if constexpr (CG == 1) {
         if (args.splits > 1) {
+            if (warp < 2 || warp == B_WARP) {  // the epilogue has been through the first barrier
+                if (!args.parts_apart) cluster_arrive();
+                cluster_wait();
+            }
             cluster_arrive();
-            cluster_wait();
+            cluster_wait();  // every slice's sums are here; from now on nothing touches another CTA's memory
             // after a time-out in any CTA the sums are wrong, and the status word says so
             if (warp >= 2 && warp < B_WARP) {
                 int tm, tn;
@@ -875,16 +894,16 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                 const int64_t m0 = (int64_t)tm * ROWS;
                 const int columns = EPI == EPI_GATED ? block_n >> 1 : block_n;
                 const int n0 = EPI == EPI_GATED ? tn * columns : (tn - which * args.n_tiles) * block_n;
-                const int groups = columns / 8;
+                const Share share(args, EPI == EPI_GATED);
+                const int groups = share.columns / 8;
                 const int rows = (int)min((int64_t)ROWS, args.M - m0);
-                const uint32_t pitch = (uint32_t)(block_n + 4) * 4u;
-                constexpr int WORKERS = 32 * EPI_WARPS;
-                for (int item = (int)slice * WORKERS + (int)threadIdx.x - 64; item < rows * groups; item += WORKERS * args.splits) {
-                    const int row = item / groups, col = (item - row * groups) * 8;
-                    const uint32_t at = stage_base + (uint32_t)row * pitch + (uint32_t)col * 4u;
+                const uint32_t plane = (uint32_t)(share.at(0, 1, 0) * 4), step = (uint32_t)(share.at(1, 0, 0) * 4);
+                for (int item = (int)threadIdx.x - 64; item < rows * groups; item += 32 * EPI_WARPS) {
+                    const int row = item / groups, own = (item - row * groups) * 8, col = (int)slice * share.columns + own;
+                    const uint32_t at = parts_base + (uint32_t)(share.at(0, 0, row) + own) * 4u;
                     uint32_t first[8], second[8];
-                    pull_parts<KIND>(at, args.splits, first);
-                    if (EPI == EPI_GATED) pull_parts<KIND>(at + (uint32_t)columns * 4u, args.splits, second);
+                    sum_parts<KIND>(at, step, args.splits, first);
+                    if (EPI == EPI_GATED) sum_parts<KIND>(at + plane, step, args.splits, second);
                     finish<P, EPI, 8>(args, which, m0 + row, n0 + col, first, second);
                 }
             }
@@ -894,7 +913,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
     // ---------------------------------------------------------------- teardown
     tc_fence_before();
     __syncthreads();
-    if (CG == 2 || args.splits > 1) {  // nobody leaves while another may still signal or read its shared memory
+    if (CG == 2) {  // nobody leaves while another may still signal its barriers
         cluster_arrive();
         cluster_wait();
     }
@@ -1116,10 +1135,16 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     a.dev_status = ctx->dev_status;
     const int own_n = c.block_n / c.cg;
     const int stage_bytes = p.planes * (c.subs * A_BYTES + own_n * 128);
-    const int slabs = EPI_WARPS * (p.planes == 3 || p.epilogue == EPI_GATED ? 0 : p.epilogue == EPI_GRAD ? SLAB_BYTES<1, EPI_GRAD> : SLAB_BYTES<1, EPI_STORE>);
-    const int stages = (tile::SMEM_LIMIT - 2048 - 1024 - slabs) / stage_bytes;
+    const int slabs = EPI_WARPS * (p.planes == 3 || p.epilogue == EPI_GATED || c.splits > 1 ? 0 : p.epilogue == EPI_GRAD ? SLAB_BYTES<1, EPI_GRAD> : SLAB_BYTES<1, EPI_STORE>);
+    int room = tile::SMEM_LIMIT - 2048 - 1024 - slabs;
+    // Room of their own for the slices' sums where it is small; otherwise they take that of the stages, once all MMAs have read them (164 KB at
+    // most, of 192 and more).
+    const int parts = c.splits > 1 ? Share(a, p.epilogue == EPI_GATED).bytes(c.splits) : 0;
+    a.parts_apart = parts > 0 && parts <= stage_bytes && p.planes == 1;
+    if (a.parts_apart) room -= parts;
+    const int stages = room / stage_bytes;
     a.stages = stages < MAX_STAGES ? stages : MAX_STAGES;
-    const size_t smem = 1024 + (size_t)a.stages * stage_bytes + slabs;
+    const size_t smem = 1024 + (size_t)a.stages * stage_bytes + slabs + (a.parts_apart ? parts : 0);
     Maps maps;
     tfjsb_status st;
     const int b_rows = p.epilogue == EPI_GATED ? c.block_n / 2 : own_n;
