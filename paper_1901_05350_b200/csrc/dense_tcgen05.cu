@@ -20,9 +20,11 @@
 // latency: a launch, the first copies (2 us) and the epilogue.
 // Persistent over tiles in bands of `band` tile rows, so that the tiles in flight share operand rows and columns in L2.
 //
-// Few tiles: K is cut among the CTAs of a cluster (CG = 1, one tile each).  Each writes its partial tile to its own shared
-// memory, and after a cluster barrier every CTA adds the parts of its share of the tile in the order of the slices, from
-// distributed shared memory, and runs the epilogue on them.  No atomics: results do not depend on scheduling.
+// Few tiles: K is cut among the CTAs of a cluster (CG = 1, one tile each).  Each has a share of the tile's columns to finish and gets the
+// other slices' sums of them written into its shared memory, which it adds, after a cluster barrier, in the order of the slices: no
+// atomics, results do not depend on scheduling.  (Sums left where they are made and read from there cost a round trip more: 64 x 512 x 2048 on
+// eight slices 10.2 us, now 7.3.  Blocks of half the registers and shared memory, so that the next kernel's could begin
+// beside them, made 1000 x 1024 x 2730 in training 120 us instead of 106: blocks come to lie two on an SM beside empty ones.)
 //
 // fp32: v = p0 + p1 + p2 (bfloat16, rounded to nearest each, exact), a b = p0 q0 + (p0 q1 + p1 q0 + p1 q1 + p0 q2 + p2 q0), what is left out is
 // below 2^-26 of it.  The tensor core cuts every sum towards zero, so the error of an accumulator grows with the number of
@@ -357,7 +359,8 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
         cluster_wait();
     }
     tc_fence_after();
-    if (CG == 1 && args.splits > 1 && args.parts_apart) cluster_arrive();  // "has begun": others may put their sums here
+    if (CG == 1 && args.splits > 1 && args.parts_apart)  // "has begun": others may put their sums here
+        asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
     const uint32_t tmem_base = tmem_base_slot;
     // Each role waits for the kernel before on its own: the producers only where that kernel may still write what they read (args.early_*), the
     // epilogue always, before it reads or writes anything, and the next kernel is let go after that wait.  So when a kernel of a chain
@@ -1017,8 +1020,8 @@ int64_t tiles_of(const Product& p, int cg, int block_n, int subs = 1) {
 //     with two parts fetches three tiles for two, a pair half of B, single CTAs everything;
 //   - the first k-block arrives, and the epilogue takes, so long; with one part a tile the epilogue runs beside the next tile's K
 //     loop, with two it holds up the next tile (by more than itself: tensor memory is read while both parts' MMAs write it);
-//   - slices cost two cluster barriers and a round trip for each share of the tile that a thread adds; clusters of more CTAs, each with an SM
-//     of its own in one group of SMs, also start later.
+//   - slices cost a cluster barrier and the exchange of the sums; clusters of more CTAs, each with an SM of its own in one group of SMs, also
+//     start later.
 double cost(const Product& p, const Shape& c, int sm_count) {
     const Args& a = p.args;
     const int kb = (a.K + (p.kind == KIND_BF16 ? 63 : 127)) / (p.kind == KIND_BF16 ? 64 : 128) * a.passes, own_kb = (kb + c.splits - 1) / c.splits;
@@ -1036,7 +1039,7 @@ double cost(const Product& p, const Shape& c, int sm_count) {
     const int64_t tiles = tiles_of(p, c.cg, c.block_n, c.subs), slots = sm_count / c.cg;
     if (c.splits > 1) {
         const int64_t shares = (int64_t)rows * (columns / 8), each = 32 * EPI_WARPS * c.splits;
-        return first + main + (c.splits == 2 ? 2100 : c.splits == 4 ? 5700 : 9700) + (double)((shares + each - 1) / each) * 2950;
+        return first + main + (c.splits == 2 ? 1400 : 5000) + (double)((shares + each - 1) / each) * 2950;
     }
     const int64_t rounds = tiles / slots, rest = tiles % slots;
     if (c.subs == 2) {

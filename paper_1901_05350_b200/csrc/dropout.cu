@@ -202,37 +202,42 @@ __global__ void __launch_bounds__(BLOCK) dropout_kernel(const __grid_constant__ 
 // A mask shared by many positions: [outer][positions][channels], one row of the mask for all positions of an outer index (spatial dropout of
 // a sequence or an image).  A thread has four channels, whose words it makes once, of `share` positions: next to no arithmetic is left, so
 // this is bound by memory where making each word again was bound by the generator (64 x 197 x 771 fp32: 28 us).  VECTOR: rows of
-// channels are whole groups of four, which a thread loads at once.  Otherwise a warp has 128 channels, a thread every 32nd of them, whose words
-// come from the threads that made them (four neighbours a thread, value by value, kept an SM's loads busy with four lines each:
-// 64 x 197 x 771 fp32 19 us).
+// channels are whole groups of four, which a thread loads at once.  Otherwise a warp has 124 channels, a thread every 32nd of them: their words
+// lie in 32 blocks wherever the first begins, a block a thread (four neighbours a thread, value by value, kept an SM's loads busy with four
+// lines each and took two or three blocks: 64 x 197 x 771 fp32 19 us, now 11.3).
 struct Positions {
-    int64_t outer, positions, groups;  // groups of four channels, or (not VECTOR) of 128
+    int64_t outer, positions, groups;  // groups of four channels, or (not VECTOR) of 124
     int share;
 };
 template <bool F32, bool RESIDUAL, bool VECTOR>
 __global__ void __launch_bounds__(BLOCK) dropout_positions_kernel(const __grid_constant__ DropoutArgs a, const __grid_constant__ Positions s) {
     ptx::pdl_wait();
-    constexpr int NEXT = VECTOR ? 1 : 32;  // from one channel of a thread to the next
+    constexpr int NEXT = VECTOR ? 1 : 32, GROUP = VECTOR ? 4 : 124;  // from one channel of a thread to the next; channels of a group
     const int lane = threadIdx.x & 31;
     const int64_t t = (int64_t)blockIdx.x * BLOCK + threadIdx.x, g = VECTOR ? t : t >> 5, o = g / s.groups;
     if (o >= s.outer) return;  // not VECTOR: all of a warp
-    const int64_t channels = (int64_t)a.extent[0], c = (g - o * s.groups) * (VECTOR ? 4 : 128) + (VECTOR ? 0 : lane);
-    const int left = VECTOR ? 4 : (int)((channels - c + 31) / 32);
-    uint64_t m = (uint64_t)(VECTOR ? c : c + 3 * lane), rest = (uint64_t)o;
+    const int64_t channels = (int64_t)a.extent[0], group = (g - o * s.groups) * GROUP, c = group + (VECTOR ? 0 : lane);
+    const int64_t end = channels - group < GROUP ? channels : group + GROUP;  // of the group
+    uint64_t m = (uint64_t)group, rest = (uint64_t)o;
     for (int d = 2; d < a.dims; ++d) {
         const uint64_t q = rest / a.extent[d];
         m += (rest - q * a.extent[d]) * a.step[d];
         rest = q;
     }
-    uint32_t w[8];
-    run_of_words<false>(a, m, w);
+    uint32_t w[4];
+    philox<false>(a, (m >> 2) + (VECTOR ? 0 : lane), w);
     bool keep[4];
+    int left = 4;
 #pragma unroll
     for (int e = 0; e < 4; ++e) keep[e] = w[e] >= a.threshold;
-    if (!VECTOR) {  // channel lane + 32 e of the warp's is value lane % 4 of thread 8 e + lane / 4
+    if (!VECTOR) {
         const uint32_t own = (keep[0] ? 1u : 0u) | (keep[1] ? 2u : 0u) | (keep[2] ? 4u : 0u) | (keep[3] ? 8u : 0u);
+        left = c < end ? (int)((end - c + 31) / 32) : 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) keep[e] = __shfl_sync(0xffffffffu, own, 8 * e + (lane >> 2)) >> (lane & 3) & 1u;
+        for (int e = 0; e < 4; ++e) {  // word i of the group's first block and those after it
+            const int i = (int)(m & 3u) + lane + 32 * e;
+            keep[e] = __shfl_sync(0xffffffffu, own, i >> 2) >> (i & 3) & 1u;
+        }
     }
     const int64_t first = (int64_t)blockIdx.y * s.share, last = first + s.share < s.positions ? first + s.share : s.positions;
     auto load4 = [&](const void* p, int64_t i, float (&v)[4]) {
@@ -307,7 +312,7 @@ cudaError_t launch_any(const DropoutArgs& a, int sm_count, cudaStream_t s) {
         Positions p;
         p.positions = (int64_t)a.extent[1];
         const bool vector = a.extent[0] % 4 == 0;
-        p.groups = ((int64_t)a.extent[0] + (vector ? 3 : 127)) / (vector ? 4 : 128);
+        p.groups = ((int64_t)a.extent[0] + (vector ? 3 : 123)) / (vector ? 4 : 124);
         p.outer = a.n / (int64_t)(a.extent[0] * a.extent[1]);
         const int64_t threads = p.outer * p.groups * (vector ? 1 : 32), blocks = (threads + BLOCK - 1) / BLOCK;
         p.share = 32;
