@@ -53,6 +53,7 @@ constexpr int EPI_WARPS = 16;  // four for each quadrant of tensor-memory lanes
 constexpr int B_WARP = 2 + EPI_WARPS;
 constexpr int THREADS = 32 * (B_WARP + 1);  // producer warp of A, MMA warp, epilogue warps, producer warp of B
 constexpr int MAX_STAGES = 8;
+constexpr int STAGES_AT_LEAST = 192 * 1024;  // bytes of all stages, whatever a tile's columns and planes
 constexpr int ROWS = 128;     // of a CTA's tile
 constexpr int A_BYTES = ROWS * 128;
 constexpr int GROUP_BYTES = 64 * 128;  // a box of 64 k x 64 columns
@@ -117,12 +118,12 @@ __device__ __forceinline__ void ld_columns(uint32_t at, uint32_t (&r)[8]) { tc_l
 // Where the slices of a tile (few tiles, K cut among the CTAs of a cluster) put their sums: the tile's columns are shared out among the CTAs, and
 // each has room for its share of every slice's rows, in rows of `pitch` values; a gated tile's for g and then for u.
 struct Share {
-    int columns, pitch, rows, planes;  // of a CTA's share
-    __host__ __device__ Share(const Args& a, bool gated) {
+    int columns, pitch, rows, planes;  // of a CTA's share; the last CTAs' may be smaller, or nothing
+    __host__ __device__ Share(int block_n, int splits, int M, bool gated) {
         planes = gated ? 2 : 1;
-        columns = a.block_n / planes / a.splits;
+        columns = (block_n / planes / 8 + splits - 1) / splits * 8;
         pitch = columns + 4;  // consecutive rows start in other banks
-        rows = a.M < ROWS ? a.M : ROWS;
+        rows = M < ROWS ? M : ROWS;
     }
     __host__ __device__ int at(int slice, int plane, int row) const { return ((slice * planes + plane) * rows + row) * pitch; }
     __host__ __device__ int bytes(int slices) const { return at(slices, 0, 0) * 4; }
@@ -848,7 +849,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                     if (!args.parts_apart) cluster_arrive();
                     cluster_wait();
                     if (ok && m0 + quad * 32 < args.M) {
-                        const Share share(args, EPI == EPI_GATED);
+                        const Share share(block_n, args.splits, args.M, EPI == EPI_GATED);
                         const int columns = EPI == EPI_GATED ? block_n >> 1 : block_n;
 #pragma unroll 1
                         for (int j = 0; part + PARTS * j < block_n / 16; ++j) {
@@ -897,8 +898,8 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                 const int64_t m0 = (int64_t)tm * ROWS;
                 const int columns = EPI == EPI_GATED ? block_n >> 1 : block_n;
                 const int n0 = EPI == EPI_GATED ? tn * columns : (tn - which * args.n_tiles) * block_n;
-                const Share share(args, EPI == EPI_GATED);
-                const int groups = share.columns / 8;
+                const Share share(block_n, args.splits, args.M, EPI == EPI_GATED);
+                const int groups = max(0, min(share.columns, columns - (int)slice * share.columns)) / 8;
                 const int rows = (int)min((int64_t)ROWS, args.M - m0);
                 const uint32_t plane = (uint32_t)(share.at(0, 1, 0) * 4), step = (uint32_t)(share.at(1, 0, 0) * 4);
                 for (int item = (int)threadIdx.x - 64; item < rows * groups; item += 32 * EPI_WARPS) {
@@ -1014,14 +1015,14 @@ int64_t tiles_of(const Product& p, int cg, int block_n, int subs = 1) {
     return ((p.args.M + rows - 1) / rows) * ((p.args.N + columns - 1) / columns) * p.args.outputs;
 }
 
-// Estimated cycles, with constants fitted to 2200 measured times of products from 10 x 128 x 192 to 13248 x 256 x 2595 on every kernel shape (the shape
-// with the least estimate takes 1 % longer than the best in the mean, 13 % at most):
+// Estimated cycles, with constants fitted to 3600 measured times of products from 10 x 128 x 192 to 13248 x 256 x 2595 on every kernel shape (the shape
+// with the least estimate takes 1 % longer than the best in the mean, 19 % at most):
 //   - a k-block takes what its MMAs take, what an SM can fetch (48 to 63 bytes a cycle) or what issuing takes, whichever is longest; a pair
 //     with two parts fetches three tiles for two, a pair half of B, single CTAs everything;
 //   - the first k-block arrives, and the epilogue takes, so long; with one part a tile the epilogue runs beside the next tile's K
 //     loop, with two it holds up the next tile (by more than itself: tensor memory is read while both parts' MMAs write it);
-//   - slices cost a cluster barrier and the exchange of the sums; clusters of more CTAs, each with an SM of its own in one group of SMs, also
-//     start later.
+//   - slices cost a cluster barrier, the sums on their way to the CTAs that add them, and the adding; clusters of more CTAs, each with an SM of
+//     its own in one group of SMs, also start later.
 double cost(const Product& p, const Shape& c, int sm_count) {
     const Args& a = p.args;
     const int kb = (a.K + (p.kind == KIND_BF16 ? 63 : 127)) / (p.kind == KIND_BF16 ? 64 : 128) * a.passes, own_kb = (kb + c.splits - 1) / c.splits;
@@ -1038,8 +1039,8 @@ double cost(const Product& p, const Shape& c, int sm_count) {
     const double epilogue = columns / 4 * column * (p.planes == 3 ? 5 : 1);
     const int64_t tiles = tiles_of(p, c.cg, c.block_n, c.subs), slots = sm_count / c.cg;
     if (c.splits > 1) {
-        const int64_t shares = (int64_t)rows * (columns / 8), each = 32 * EPI_WARPS * c.splits;
-        return first + main + (c.splits == 2 ? 1400 : 5000) + (double)((shares + each - 1) / each) * 2950;
+        const int64_t items = (int64_t)rows * ((columns / 8 + c.splits - 1) / c.splits), threads = 32 * EPI_WARPS;  // eight columns each
+        return first + main + 1200 + 430 * c.splits + 0.25 * rows * c.block_n * (c.splits - 1) / c.splits + (double)((items + threads - 1) / threads) * 1800;
     }
     const int64_t rounds = tiles / slots, rest = tiles % slots;
     if (c.subs == 2) {
@@ -1052,11 +1053,9 @@ double cost(const Product& p, const Shape& c, int sm_count) {
 
 // Clusters of that many CTAs, one to an SM, that are resident at once: less than the SMs over their number, which the GPU's groups of SMs
 // do not divide.
-int resident_clusters(int size) {
+int resident_clusters(int dev, int size) {
     constexpr int DEVICES = 64;
     static std::atomic<int> known[DEVICES][9];  // 0: not asked yet
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
     if (dev < DEVICES)
         if (const int n = known[dev][size].load(std::memory_order_relaxed)) return n;
     auto* kernel = &dense_kernel<1, 1, KIND_BF16, EPI_STORE, 1, false, false>;
@@ -1081,7 +1080,7 @@ int resident_clusters(int size) {
     return n;
 }
 
-Shape choose(const Product& p, int sm_count) {
+Shape choose(const Product& p, int dev, int sm_count) {
     const char* forced = getenv("TFJSB_DENSE_SHAPE");  // for tests: "CTA group,columns,slices,parts", wherever the product allows it
     int f[4];
     const bool force = forced && sscanf(forced, "%d,%d,%d,%d", &f[0], &f[1], &f[2], &f[3]) == 4;
@@ -1093,10 +1092,12 @@ Shape choose(const Product& p, int sm_count) {
             if (p.planes == 3 && bn != 128) continue;                         // two accumulators of 128 columns, two stages
             if (bn == 64 && (cg == 2 || p.epilogue == EPI_GATED)) continue;   // boxes are 64 columns wide
             const int64_t tiles = tiles_of(p, cg, bn);
-            for (int splits = 1; splits <= (cg == 1 ? 8 : 1); splits *= 2) {
-                // at least four k-blocks a slice, none without any, one wave
+            for (int splits = 1; splits <= (cg == 1 ? 8 : 1); ++splits) {
+                // at least four k-blocks a slice, none without any, one wave, and room for the sums
                 const int each = (kb + splits - 1) / splits;
-                if (splits > 1 && (each < 4 || each * (splits - 1) >= kb || tiles * splits > sm_count || tiles > resident_clusters(splits))) continue;
+                if (splits > 1 && (each < 4 || each * (splits - 1) >= kb || tiles * splits > sm_count || tiles > resident_clusters(dev, splits) ||
+                                   Share(bn, splits, p.args.M, p.epilogue == EPI_GATED).bytes(splits) > STAGES_AT_LEAST))
+                    continue;
                 for (int subs = 1; subs <= (cg == 2 && bn == 256 && p.planes == 1 ? 2 : 1); ++subs) {
                     const Shape c = {cg, bn, splits, subs};
                     if (force && f[0] == cg && f[1] == bn && f[2] == splits && f[3] == subs) return c;
@@ -1113,7 +1114,7 @@ Shape choose(const Product& p, int sm_count) {
 tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     if (!ctx->encode_tiled) return fail(ctx, TFJSB_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
     Args& a = p.args;
-    const Shape c = choose(p, ctx->sm_count);
+    const Shape c = choose(p, ctx->device, ctx->sm_count);
     const int bk = p.kind == KIND_BF16 ? 64 : 128;
     a.block_n = c.block_n;
     a.splits = c.splits;
@@ -1140,9 +1141,8 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     const int stage_bytes = p.planes * (c.subs * A_BYTES + own_n * 128);
     const int slabs = EPI_WARPS * (p.planes == 3 || p.epilogue == EPI_GATED || c.splits > 1 ? 0 : p.epilogue == EPI_GRAD ? SLAB_BYTES<1, EPI_GRAD> : SLAB_BYTES<1, EPI_STORE>);
     int room = tile::SMEM_LIMIT - 2048 - 1024 - slabs;
-    // Room of their own for the slices' sums where it is small; otherwise they take that of the stages, once all MMAs have read them (164 KB at
-    // most, of 192 and more).
-    const int parts = c.splits > 1 ? Share(a, p.epilogue == EPI_GATED).bytes(c.splits) : 0;
+    // Room of their own for the slices' sums where it is small; otherwise they take that of the stages, once all MMAs have read them.
+    const int parts = c.splits > 1 ? Share(c.block_n, c.splits, a.M, p.epilogue == EPI_GATED).bytes(c.splits) : 0;
     a.parts_apart = parts > 0 && parts <= stage_bytes && p.planes == 1;
     if (a.parts_apart) room -= parts;
     const int stages = room / stage_bytes;

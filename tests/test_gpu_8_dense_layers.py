@@ -590,3 +590,24 @@ def test_what_was_saved_is_checked(ctx):
         with pytest.raises(ValueError):
             ctx.gated_ffn_backprop(x, wg, wu, wd, h, z, dy, want=want)
     assert ctx.launch_count == before
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("columns,slices", [(c, s) for c in (64, 128, 256) for s in (3, 5, 6, 7)], ids=str)
+def test_slices_whose_shares_differ(ctx, monkeypatch, columns, slices, dtype):
+    """K cut in numbers that do not divide a tile's columns: some CTAs finish fewer of them, or none."""
+    monkeypatch.setenv("TFJSB_DENSE_SHAPE", f"1,{columns},{slices},1")
+    for shape in ((37, 2000, 456, 100), (130, 1900, 250, 72), (250, 328, 3000, 136)):
+        x, wg, wu, wd, dy = block(400 + columns + slices, *shape, dtype)
+        y, h, z = ctx.gated_ffn(x, wg, wu, wd, save=True)
+        grads = ctx.gated_ffn_backprop(x, wg, wu, wd, h, z, dy)
+        ctx.check_device_status()
+        want = [ref.gated_ffn(x, wg, wu, wd, "silu"), *ref.gated_ffn_gradients(x, wg, wu, wd, dy, "silu")]
+        bounds = ref.gated_ffn_bounds(x, wg, wu, wd, dy, "silu")
+        for got, w, b, what in zip((y, *grads), want, bounds, ("y", "dx", "dw_gate", "dw_up", "dw_down")):
+            check_ffn(got, w, b, dtype, what)
+    if dtype == torch.float32:
+        q, s = ctx.quantize_int8(normal(1, (200, 5000)))
+        a, sa = ctx.quantize_int8(normal(2, (70, 5000)))
+        want, bound = ref.int8_product(a, sa, q, s, None, "none")
+        assert ((ctx.matmul_int8(a, sa, q, s, out_dtype=torch.float32).double() - want).abs() <= bound).all()
