@@ -68,11 +68,11 @@ constexpr int few_rows_ffn(bool f32) { return f32 ? FEW_ROWS : 2; }
 tfjsb_status few_rows_gated(tfjsb_ctx* ctx, bool f32, const void* x, const void* w_gate, const void* w_up, int gate, float* h, int64_t rows, int64_t N,
                             int64_t K, cudaStream_t s);
 tfjsb_status few_rows_down(tfjsb_ctx* ctx, bool f32, const float* h, const void* w, void* y, int64_t rows, int64_t N, int64_t K, cudaStream_t s);
-// One row of 8-bit products.  x_kind: 0 8-bit values [K rounded up to 16] with a_scale, 1 bfloat16, 2 fp32.  (With two and four rows
-// 4096 x 4096 took 8.2 and 11.3 us this way, 8.3 for eight rows on the tensor cores.)
+// 8-bit products of rows that are quantised by the same kernel.  x_kind: 0 one row of 8-bit values [K rounded up to 16] with
+// a_scale, 1 bfloat16, 2 fp32.  More than one row: M max(N, K) below 2^32.
 constexpr int ROW_INT8_BYTES = 131072;  // of the largest K: the row's 8-bit values are in shared memory
-tfjsb_status row_int8(tfjsb_ctx* ctx, int x_kind, const void* x, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias, int act,
-                      void* out, bool out_bf16, int64_t N, int64_t K, cudaStream_t s);
+tfjsb_status rows_int8(tfjsb_ctx* ctx, int x_kind, const void* x, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias, int act,
+                      void* out, bool out_bf16, int64_t M, int64_t N, int64_t K, cudaStream_t s);
 
 // The context's device is the current one while this lives: tensors say where they are, the caller's device may be another.
 struct OnDevice {

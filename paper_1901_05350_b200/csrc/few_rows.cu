@@ -6,8 +6,8 @@
 // order through shared and distributed shared memory.
 //
 //   matrices [K, N] (the gated block): a block has 64 columns, a thread 8 of them and every 32nd k; K is cut among the CTAs of a cluster
-//   matrices [N, K] of 8-bit integers, one row of x: a warp has a row of weights, a lane 16 bytes of each 512; the row of x is quantised, or
-//   copied, into shared memory by every block
+//   matrices [N, K] of 8-bit integers: a block has one row of x, which it quantises, or copies, into shared memory; a warp has a row of
+//   weights, a lane 16 bytes of each 512
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -222,9 +222,9 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(const __grid_constant
 }
 
 template <typename... KArgs, typename... A>
-cudaError_t launch_clusters(void (*kernel)(KArgs...), int64_t grid, int cluster, size_t smem, cudaStream_t s, int64_t* launches, A&&... args) {
+cudaError_t launch_clusters(void (*kernel)(KArgs...), dim3 grid, int cluster, size_t smem, cudaStream_t s, int64_t* launches, A&&... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -256,7 +256,7 @@ cudaError_t launch_few(const FewArgs& a, bool vector, int64_t grid, cudaStream_t
     auto* kernel = vector ? &few_rows_kernel<F32, X32, GATED, T, true> : &few_rows_kernel<F32, X32, GATED, T, false>;
     const cudaError_t e = smem_attr_once(reinterpret_cast<const void*>(kernel), CHUNK * T * 4);
     if (e != cudaSuccess) return e;
-    return launch_clusters(kernel, grid, a.splits, smem, s, launches, a);
+    return launch_clusters(kernel, dim3((unsigned)grid), a.splits, smem, s, launches, a);
 }
 
 template <bool F32, bool X32, bool GATED>
@@ -280,7 +280,7 @@ tfjsb_status few(tfjsb_ctx* ctx, const void* x, const void* w0, const void* w1, 
 // ---- 8-bit weights -------------------------------------------------------------------------------------------
 
 struct FewInt8Args {
-    const void* x;         // QUANTIZE: K values; otherwise [pitch] 8-bit
+    const void* x;         // QUANTIZE: rows of K values; otherwise [pitch] 8-bit
     const float* a_scale;  // not with QUANTIZE
     const int8_t* bt;      // [N, pitch]
     const float *b_scale, *bias;
@@ -289,7 +289,7 @@ struct FewInt8Args {
     int K, pitch, act, out_bf16;
 };
 
-// One row of x.  QUANTIZE: 0 x is 8-bit already, 1 bfloat16, 2 fp32.
+// A row of x for every blockIdx.y.  QUANTIZE: 0 x is 8-bit already (one row), 1 bfloat16, 2 fp32.
 template <int QUANTIZE>
 __global__ void __launch_bounds__(THREADS, 4) few_rows_int8_kernel(const __grid_constant__ FewInt8Args a) {
     extern __shared__ __align__(16) int8_t q[];  // [pitch]
@@ -297,6 +297,7 @@ __global__ void __launch_bounds__(THREADS, 4) few_rows_int8_kernel(const __grid_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
     pdl_launch_dependents();
+    const uint32_t x_at = QUANTIZE == 0 ? 0u : blockIdx.y * (uint32_t)a.K;  // several rows are small layers'
     constexpr int U = 8;     // pieces of 512 bytes of a row of weights in flight a warp
     constexpr int HELD = 2;  // groups of eight values of x that a thread holds between the maximum and the rounding
     const int64_t step = (int64_t)gridDim.x * WARPS;
@@ -324,7 +325,7 @@ __global__ void __launch_bounds__(THREADS, 4) few_rows_int8_kernel(const __grid_
             const int k = (j * THREADS + threadIdx.x) * 8;
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[j][e] = 0.f;
-            if (k < a.K) values8<QUANTIZE == 2>(a.x, k, left_at(k), v[j]);
+            if (k < a.K) values8<QUANTIZE == 2>(a.x, (int64_t)(x_at + k), left_at(k), v[j]);
         }
 #pragma unroll
         for (int j = 0; j < HELD; ++j)
@@ -332,7 +333,7 @@ __global__ void __launch_bounds__(THREADS, 4) few_rows_int8_kernel(const __grid_
             for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(v[j][e]));
         for (int k = (HELD * THREADS + threadIdx.x) * 8; k < a.K; k += THREADS * 8) {
             float more[8];
-            values8<QUANTIZE == 2>(a.x, k, left_at(k), more);
+            values8<QUANTIZE == 2>(a.x, (int64_t)(x_at + k), left_at(k), more);
 #pragma unroll
             for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(more[e]));
         }
@@ -352,7 +353,7 @@ __global__ void __launch_bounds__(THREADS, 4) few_rows_int8_kernel(const __grid_
         }
         for (int k = (HELD * THREADS + threadIdx.x) * 8; k < a.pitch; k += THREADS * 8) {
             float more[8] = {};
-            if (k < a.K) values8<QUANTIZE == 2>(a.x, k, left_at(k), more);
+            if (k < a.K) values8<QUANTIZE == 2>(a.x, (int64_t)(x_at + k), left_at(k), more);
             *reinterpret_cast<uint2*>(q + k) = quantize8<QUANTIZE == 2>(more, rs);
         }
     }
@@ -379,20 +380,21 @@ __global__ void __launch_bounds__(THREADS, 4) few_rows_int8_kernel(const __grid_
             // as the tensor-core product's epilogue does it, to the bit
             float v = fmaf((float)sum * scale, load_global(a.b_scale + n), a.bias ? load_global(a.bias + n) : 0.f);
             v = apply_act(v, a.act);
-            if (a.out_bf16) static_cast<__nv_bfloat16*>(a.out)[n] = __float2bfloat16_rn(v);
-            else static_cast<float*>(a.out)[n] = v;
+            const int64_t at = n + (QUANTIZE == 0 ? 0 : (int64_t)(blockIdx.y * (uint32_t)a.N));
+            if (a.out_bf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
+            else static_cast<float*>(a.out)[at] = v;
         }
     }
 }
 
 template <int QUANTIZE>
-cudaError_t launch_int8(const FewInt8Args& a, int sm_count, cudaStream_t s, int64_t* launches) {
+cudaError_t launch_int8(const FewInt8Args& a, int64_t rows, int sm_count, cudaStream_t s, int64_t* launches) {
     auto* kernel = &few_rows_int8_kernel<QUANTIZE>;
     const cudaError_t e = smem_attr_once(reinterpret_cast<const void*>(kernel), ROW_INT8_BYTES);
     if (e != cudaSuccess) return e;
     // a row of weights a warp; blocks of 64 registers a thread are four to an SM
-    const int64_t needed = (a.N + WARPS - 1) / WARPS, most = (int64_t)sm_count * 4;
-    return launch_clusters(kernel, needed < most ? needed : most, 1, (size_t)a.pitch, s, launches, a);
+    const int64_t needed = (a.N + WARPS - 1) / WARPS, most = rows < (int64_t)sm_count * 4 ? sm_count * 4 / rows : 1;
+    return launch_clusters(kernel, dim3((unsigned)(needed < most ? needed : most), (unsigned)rows), 1, (size_t)a.pitch, s, launches, a);
 }
 
 }  // namespace
@@ -405,13 +407,13 @@ tfjsb_status few_rows_down(tfjsb_ctx* ctx, bool f32, const float* h, const void*
     return f32 ? few<true, true, false>(ctx, h, w, nullptr, 0, y, rows, N, K, s) : few<false, true, false>(ctx, h, w, nullptr, 0, y, rows, N, K, s);
 }
 
-tfjsb_status row_int8(tfjsb_ctx* ctx, int x_kind, const void* x, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias, int act,
-                      void* out, bool out_bf16, int64_t N, int64_t K, cudaStream_t s) {
+tfjsb_status rows_int8(tfjsb_ctx* ctx, int x_kind, const void* x, const float* a_scale, const int8_t* bt, const float* b_scale, const float* bias, int act,
+                      void* out, bool out_bf16, int64_t M, int64_t N, int64_t K, cudaStream_t s) {
     const FewInt8Args a = {x, a_scale, bt, b_scale, bias, out, N, (int)K, (int)((K + 15) / 16 * 16), act, out_bf16 ? 1 : 0};
-    const cudaError_t e = x_kind == 0   ? launch_int8<0>(a, ctx->sm_count, s, &ctx->launches)
-                          : x_kind == 1 ? launch_int8<1>(a, ctx->sm_count, s, &ctx->launches)
-                                        : launch_int8<2>(a, ctx->sm_count, s, &ctx->launches);
-    return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "8-bit row launch");
+    const cudaError_t e = x_kind == 0   ? launch_int8<0>(a, M, ctx->sm_count, s, &ctx->launches)
+                          : x_kind == 1 ? launch_int8<1>(a, M, ctx->sm_count, s, &ctx->launches)
+                                        : launch_int8<2>(a, M, ctx->sm_count, s, &ctx->launches);
+    return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "8-bit rows launch");
 }
 
 }  // namespace dense

@@ -611,3 +611,44 @@ def test_slices_whose_shares_differ(ctx, monkeypatch, columns, slices, dtype):
         a, sa = ctx.quantize_int8(normal(2, (70, 5000)))
         want, bound = ref.int8_product(a, sa, q, s, None, "none")
         assert ((ctx.matmul_int8(a, sa, q, s, out_dtype=torch.float32).double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("shape", [(2, 5, 17), (7, 1930, 36), (31, 410, 106), (64, 90, 2047), (300, 11, 33), (2000, 5, 100), (12000, 1, 16), (3, 3, 131072)], ids=str)
+def test_int8_layers_of_one_kernel(ctx, shape, dtype):
+    """Small layers quantise their rows and multiply them in one kernel: the same bits as the two calls."""
+    m, n, k = shape
+    x, bias = normal(1, (m, k), 1.0, dtype), normal(2, (n,))
+    w, w_scale = ctx.quantize_int8(normal(3, (n, k)))
+    q, scale = ctx.quantize_int8(x)
+    before = ctx.launch_count
+    y = ctx.dense_int8(x, w, w_scale, bias=bias, act="relu", out_dtype=torch.float32)
+    assert ctx.launch_count == before + (1 if m * n <= 26000000 // (k + 2048) else 2)  # 31 x 410 x 106 is just beyond
+    assert torch.equal(y, ctx.matmul_int8(q, scale, w, w_scale, bias=bias, act="relu", out_dtype=torch.float32))
+    want, bound = ref.int8_product(q, scale, w, w_scale, bias, "relu")
+    assert ((y.double() - want).abs() <= bound).all()
+
+
+def test_two_threads_on_two_streams(ctx):
+    """One context: calls share no memory, so two threads may make them at once."""
+    import threading
+
+    x, wg, wu, wd, dy = block(95, 100, 256, 520, 256, torch.bfloat16)
+    want = training_step(ctx, x, wg, wu, wd, dy, 5)
+    torch.cuda.synchronize()
+    results = [[], []]
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                results[i].append(training_step(ctx, x, wg, wu, wd, dy, 5))
+        stream.synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(results[0]) == len(results[1]) == 20
+    assert all(torch.equal(a, b) for r in results for got in r for a, b in zip(got, want))
