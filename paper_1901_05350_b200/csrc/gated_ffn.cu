@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(256) layout_kernel(const __grid_constant__ Lay
 // ---- layout of the buffers ---------------------------------------------------------------------------------
 constexpr int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
 constexpr int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
-constexpr int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
+constexpr int64_t MOST_BYTES = 1LL << 60;  // of a buffer: sums of a few of them, and addresses, stay within 64 bits
 
 struct Sizes {
     int planes;            // 1 (bfloat16) or 3 (fp32)
@@ -126,7 +126,6 @@ struct Sizes {
     bool repack_x, repack_up, repack_down, repack_dy;  // operands that are copied: x; w_gate and w_up; w_down; dy
     int64_t x_bytes, w_bytes, wd_bytes, dy_bytes;      // of such a copy
     int64_t h_bytes, z_bytes, grad_bytes;              // grad: dg and du
-    int64_t few;                                       // h of the form for few tokens, fp32
     int64_t forward, backward;
 };
 
@@ -147,18 +146,29 @@ tfjsb_status sizes_of(const tfjsb_ffn* f, Sizes* s, std::string* why) {
     s->repack_x = f32 || s->D % 8;
     s->repack_up = f32 || s->F % 8;
     s->repack_down = s->repack_dy = f32 || s->Do % 8;
-    const int64_t e = 2 * s->planes;
-    s->x_bytes = up256(s->T * up8(s->D) * e);
-    s->w_bytes = up256(s->D * up8(s->F) * e);
-    s->wd_bytes = up256(s->F * up8(s->Do) * e);
-    s->dy_bytes = up256(s->T * up8(s->Do) * e);
-    s->h_bytes = up256(s->T * s->fp * e);
-    s->z_bytes = up256((s->T + 31) / 32 * 32 * s->fp * 8);  // whole blocks of 32 rows
-    s->grad_bytes = up256(s->T * s->fp * 2 * e);
-    const int64_t weights = (s->repack_x ? s->x_bytes : 0) + (s->repack_up ? 2 * s->w_bytes : 0) + (s->repack_down ? s->wd_bytes : 0);
-    s->few = s->T <= few_rows_ffn(f32) ? up256(s->T * s->F * 4) : 0;
-    s->forward = weights + s->h_bytes > s->few ? weights + s->h_bytes : s->few;
-    s->backward = weights + (s->repack_dy ? s->dy_bytes : 0) + s->grad_bytes;
+    // Every byte count below is worked out in 128 bits first: 2^30 tokens of 2^30 hidden values have more bytes than 64 bits hold, and a
+    // count that wrapped around would let any workspace pass.
+    const __int128 e = 2 * s->planes, T = s->T;
+    const auto up = [](__int128 v) { return (v + 255) / 256 * 256; };
+    const __int128 x_bytes = up(T * up8(s->D) * e), w_bytes = up(up8(s->F) * e * s->D), wd_bytes = up(up8(s->Do) * e * s->F), dy_bytes = up(T * up8(s->Do) * e);
+    const __int128 h_bytes = up(T * s->fp * e), z_bytes = up((T + 31) / 32 * 32 * s->fp * 8), grad_bytes = up(T * s->fp * 2 * e);  // z: whole blocks of 32 rows
+    const __int128 weights = (s->repack_x ? x_bytes : 0) + (s->repack_up ? 2 * w_bytes : 0) + (s->repack_down ? wd_bytes : 0);
+    const __int128 few = T <= few_rows_ffn(f32) ? up(T * s->F * 4) : 0;
+    const __int128 forward = weights + h_bytes > few ? weights + h_bytes : few, backward = weights + (s->repack_dy ? dy_bytes : 0) + grad_bytes;
+    for (const __int128 bytes : {z_bytes, forward, backward, (__int128)s->D * s->F * e, (__int128)s->F * s->Do * e, T * s->D * e, T * s->Do * e})
+        if (bytes > MOST_BYTES) {
+            *why = "a buffer of the block would have more than 2^60 bytes";
+            return TFJSB_ERR_SHAPE;
+        }
+    s->x_bytes = (int64_t)x_bytes;
+    s->w_bytes = (int64_t)w_bytes;
+    s->wd_bytes = (int64_t)wd_bytes;
+    s->dy_bytes = (int64_t)dy_bytes;
+    s->h_bytes = (int64_t)h_bytes;
+    s->z_bytes = (int64_t)z_bytes;
+    s->grad_bytes = (int64_t)grad_bytes;
+    s->forward = (int64_t)forward;
+    s->backward = (int64_t)backward;
     return TFJSB_OK;
 }
 
