@@ -25,15 +25,19 @@
  *             Results are valid once the caller synchronises the stream.
  *   Errors    Every call returns a tfjsb_status.  All argument checks happen on the host
  *             before anything is launched; on error nothing has been enqueued.
- *             `tfjsb_last_error` gives a message for the last failing call on that context
- *             (valid until the next call on the context).  No CPU fallback exists: with no
+ *             `tfjsb_last_error` gives a message for the last failing call on that context (of the
+ *             calling thread, where it has not asked for that one yet; valid until the thread's next call
+ *             on the context).  No CPU fallback exists: with no
  *             usable CUDA device `tfjsb_init` fails with TFJSB_ERR_CUDA.
- *   Threads   A context may be used from one host thread at a time.
+ *   Threads   A context may be used from one host thread at a time.  The calls of the dense layers of transformer
+ *             blocks may be made on one context by several threads at once (while no other call is); what the status
+ *             word has to report goes to whichever thread checks it first.
  *   Streams   The kernels are written to have the GPU to themselves: persistent grids sized to all SMs,
  *             tensor memory and most of an SM's shared memory per CTA.  Enqueue the work of a process on one
  *             stream at a time, or order the streams with events; kernels of two streams that run side by
  *             side on the same SMs are not a supported configuration (copies on a second stream are fine:
- *             `tfjsb_run_model_host_async` does that itself).
+ *             `tfjsb_run_model_host_async` does that itself).  The dense layers of transformer blocks are the
+ *             exception among themselves: their kernels may run side by side on several streams.
  */
 #ifndef TFJSB_H_
 #define TFJSB_H_
@@ -274,7 +278,8 @@ tfjsb_status tfjsb_bias_backprop(tfjsb_ctx* ctx, const tfjsb_tensor* dz, tfjsb_t
  * Tensors are DEVICE pointers to dense row-major values of the stated type, 16-byte aligned; outputs may alias neither inputs
  * nor each other (dropout excepted).  Results do not depend on scheduling: the same call gives the same bits.  Workspaces are the
  * caller's, 16-byte aligned, of at least the bytes that the *_sizes / *_workspace function gives; their contents mean nothing between calls.
- * Calls whose workspaces and outputs are their own share nothing, so they can be captured into graphs of their own. */
+ * Calls whose workspaces and outputs are their own share no memory but the context's status word, so they can be captured into graphs of
+ * their own, made from several threads and run side by side on several streams. */
 
 /* A gated feed-forward block: y = (gate(x w_gate) * (x w_up)) w_down, no biases.
  *   x [tokens,width], w_gate and w_up [width,hidden], w_down [hidden,out_width], y [tokens,out_width], all of `dtype`.

@@ -16,7 +16,13 @@ namespace tfjsb {
 thread_local bool g_launch_pdl = getenv("TFJSB_NO_PDL") == nullptr;
 
 tfjsb_status fail(tfjsb_ctx* ctx, tfjsb_status st, const std::string& msg) {
-    if (ctx) ctx->last_error = msg;
+    if (ctx) {
+        std::lock_guard<std::mutex> lock(ctx->failures_lock);
+        ctx->last_failing = std::this_thread::get_id();
+        tfjsb_ctx::Failure& own = ctx->failures[ctx->last_failing];
+        own.text = msg;
+        own.unread = true;
+    }
     return st;
 }
 
@@ -256,7 +262,18 @@ tfjsb_status tfjsb_set_math(tfjsb_ctx* ctx, tfjsb_math mode) {
     return TFJSB_OK;
 }
 
-const char* tfjsb_last_error(tfjsb_ctx* ctx) { return ctx ? ctx->last_error.c_str() : "null context"; }
+const char* tfjsb_last_error(tfjsb_ctx* ctx) {
+    if (!ctx) return "null context";
+    // The text that is returned belongs to this thread: no other writes it.
+    std::lock_guard<std::mutex> lock(ctx->failures_lock);
+    tfjsb_ctx::Failure& own = ctx->failures[std::this_thread::get_id()];
+    if (!own.unread) {
+        const auto last = ctx->failures.find(ctx->last_failing);
+        if (last != ctx->failures.end() && &last->second != &own) own.text = last->second.text;
+    }
+    own.unread = false;
+    return own.text.c_str();
+}
 
 tfjsb_status tfjsb_check_device_status(tfjsb_ctx* ctx, void* stream) {
     TFJSB_REQUIRE_CTX(ctx);
@@ -275,7 +292,7 @@ tfjsb_status tfjsb_check_device_status(tfjsb_ctx* ctx, void* stream) {
     return TFJSB_OK;
 }
 
-int64_t tfjsb_launch_count(tfjsb_ctx* ctx) { return ctx ? ctx->launches : -1; }
+int64_t tfjsb_launch_count(tfjsb_ctx* ctx) { return ctx ? __atomic_load_n(&ctx->launches, __ATOMIC_RELAXED) : -1; }
 
 tfjsb_status tfjsb_window_out_shape(int64_t in, int k, int stride, int dilation, tfjsb_pad pad, int64_t* out,
                                     int* pad_before, int* pad_after) {

@@ -6,7 +6,10 @@
 #include <cuda.h>
 #include <stdint.h>
 
+#include <map>
+#include <mutex>
 #include <string>
+#include <thread>
 #include <utility>
 #include <vector>
 
@@ -119,14 +122,22 @@ struct tfjsb_ctx {
     int device = 0;
     int sm_count = 0;
     tfjsb_math math = TFJSB_MATH_TF32;
-    std::string last_error;
+    // Messages of failing calls, a thread's own each (several threads may call the dense layers at once); `unread` ones have not
+    // been asked for by their thread.
+    struct Failure {
+        std::string text;
+        bool unread = false;
+    };
+    std::mutex failures_lock;
+    std::map<std::thread::id, Failure> failures;
+    std::thread::id last_failing;
     unsigned int* dev_status = nullptr;  // device status word
     tfjsb::EncodeTiledFn encode_tiled = nullptr;
     tfjsb::EncodeIm2colFn encode_im2col = nullptr;
     tfjsb::Scratch scratch_a, scratch_b;  // transposed operands of tfjsb_matmul
     tfjsb::Scratch scratch_c;             // partial sums of the filter / bias gradients
     std::vector<void*> retired;            // outgrown scratch blocks, freed at shutdown
-    int64_t launches = 0;
+    int64_t launches = 0;                  // see count_launch
     int live_models = 0;
 };
 
@@ -134,6 +145,8 @@ namespace tfjsb {
 
 tfjsb_status fail(tfjsb_ctx* ctx, tfjsb_status st, const std::string& msg);
 tfjsb_status cuda_fail(tfjsb_ctx* ctx, cudaError_t err, const char* what);
+// One more launch, by calls that several threads may make at once.
+inline void count_launch(int64_t* launches) { __atomic_add_fetch(launches, 1, __ATOMIC_RELAXED); }
 // Grows `s` to at least `bytes`.  Never synchronises: an outgrown block may still be read by kernels in
 // flight on any stream, so it is kept until tfjsb_shutdown; growth is geometric, so all outgrown blocks
 // together are smaller than the live one.  tfjsb_reserve_scratch sizes the blocks up front.

@@ -986,7 +986,7 @@ cudaError_t launch(const Maps& maps, const Args& args, int grid, size_t smem, cu
     cfg.attrs = attr;
     cfg.numAttrs = n;
     e = cudaLaunchKernelEx(&cfg, kernel, maps, args);
-    if (e == cudaSuccess) ++*launches;
+    if (e == cudaSuccess) count_launch(launches);
     return e;
 }
 

@@ -399,7 +399,7 @@ tfjsb_status run(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, const char* x
     if (dtype == TFJSB_DTYPE_F32) e = residual ? launch_any<true, true>(a, ctx->sm_count, s) : launch_any<true, false>(a, ctx->sm_count, s);
     else e = residual ? launch_any<false, true>(a, ctx->sm_count, s) : launch_any<false, false>(a, ctx->sm_count, s);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "dropout launch");
-    ++ctx->launches;
+    count_launch(&ctx->launches);
     return TFJSB_OK;
 }
 

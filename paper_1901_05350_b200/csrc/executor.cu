@@ -613,8 +613,8 @@ tfjsb_status tfjsb_model_create(tfjsb_ctx* ctx, const tfjsb_layer_desc* layers, 
                     return bail(TFJSB_ERR_SHAPE, where + "the filter window does not fit the input under 'valid' padding");
                 step.g = g;
                 const size_t f_elems = (size_t)g.fh * g.fw * g.C * (dw ? g.mult : g.Co);
-                if ((st = upload(m, L.filter, f_elems, &step.filter)) != TFJSB_OK) return bail(st, ctx->last_error);
-                if (L.bias && (st = upload(m, L.bias, (size_t)g.Co, &step.bias)) != TFJSB_OK) return bail(st, ctx->last_error);
+                if ((st = upload(m, L.filter, f_elems, &step.filter)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
+                if (L.bias && (st = upload(m, L.bias, (size_t)g.Co, &step.bias)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
                 if (m->narrow) {
                     // what is stored is a bfloat16: the filter is rounded once, here
                     cudaError_t e = launch_round_to_bf16_in_place(step.filter, (int64_t)f_elems, 0, &ctx->launches);
@@ -678,8 +678,8 @@ tfjsb_status tfjsb_model_create(tfjsb_ctx* ctx, const tfjsb_layer_desc* layers, 
                 int64_t feat = 1;
                 for (int i = 1; i < rank; ++i) feat *= d[i];
                 step.M = d[0]; step.K = feat; step.N = L.out_channels;
-                if ((st = upload(m, L.filter, (size_t)(step.K * step.N), &step.filter)) != TFJSB_OK) return bail(st, ctx->last_error);
-                if (L.bias && (st = upload(m, L.bias, (size_t)step.N, &step.bias)) != TFJSB_OK) return bail(st, ctx->last_error);
+                if ((st = upload(m, L.filter, (size_t)(step.K * step.N), &step.filter)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
+                if (L.bias && (st = upload(m, L.bias, (size_t)step.N, &step.bias)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
                 step.kind = (m->use_tf32 && gemm_tf32_supported(step.M, step.N, step.K)) ? STEP_GEMM_TF32 : STEP_GEMM_FP32;
                 if (m->narrow) {
                     if (li == 0) return bail(TFJSB_ERR_UNSUPPORTED, where + "in the bfloat16 storage mode the first layer must be a conv2d");
@@ -719,7 +719,7 @@ tfjsb_status tfjsb_model_create(tfjsb_ctx* ctx, const tfjsb_layer_desc* layers, 
             step.conv_patch = conv_small_window_supported(step.g) && !getenv("TFJSB_NO_PATCH_CONV");
             // filter [fh*fw*Cin, Cout] -> [Cout, k_pad] once, on the device
             const int64_t k_pad = conv_igemm_k_pad(step.g);
-            if ((st = dev_alloc(m, (size_t)(k_pad * step.g.Co), &step.filter_km)) != TFJSB_OK) return bail(st, ctx->last_error);
+            if ((st = dev_alloc(m, (size_t)(k_pad * step.g.Co), &step.filter_km)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
             cudaError_t e = launch_pack_conv_filter(step.filter, step.filter_km, step.g, 0, &ctx->launches);
             if (e != cudaSuccess) return bail(TFJSB_ERR_CUDA, std::string("packing weights: ") + cudaGetErrorString(e));
         }
@@ -730,18 +730,18 @@ tfjsb_status tfjsb_model_create(tfjsb_ctx* ctx, const tfjsb_layer_desc* layers, 
             step.pack_r = r;
             const size_t w_elems = (size_t)(step.K * step.N) * r * r;
             float* km32 = nullptr;
-            if ((st = dev_alloc(m, (size_t)(step.K * step.N), &km32)) != TFJSB_OK) return bail(st, ctx->last_error);
+            if ((st = dev_alloc(m, (size_t)(step.K * step.N), &km32)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
             float* km16 = nullptr;
-            if ((st = dev_alloc(m, (w_elems + 1) / 2, &km16)) != TFJSB_OK) return bail(st, ctx->last_error);
+            if ((st = dev_alloc(m, (w_elems + 1) / 2, &km16)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
             cudaError_t e = launch_transpose(step.filter, km32, step.K, step.N, 0, &ctx->launches);
             step.filter_km = km32;  // [N, K] fp32 holding bfloat16 values: the B operand of the fused block kernel
             if (r > 1) {
                 float* diag = nullptr;
-                if ((st = dev_alloc(m, w_elems, &diag)) != TFJSB_OK) return bail(st, ctx->last_error);
+                if ((st = dev_alloc(m, w_elems, &diag)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
                 if (e == cudaSuccess) e = launch_block_diagonal(km32, diag, step.N, step.K, r, 0, &ctx->launches);
                 km32 = diag;
                 if (step.bias) {
-                    if ((st = dev_alloc(m, (size_t)step.N * r, &step.bias_packed)) != TFJSB_OK) return bail(st, ctx->last_error);
+                    if ((st = dev_alloc(m, (size_t)step.N * r, &step.bias_packed)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
                     for (int j = 0; j < r && e == cudaSuccess; ++j)
                         e = cudaMemcpy(step.bias_packed + (size_t)j * step.N, step.bias, (size_t)step.N * 4, cudaMemcpyDeviceToDevice);
                 }
@@ -752,7 +752,7 @@ tfjsb_status tfjsb_model_create(tfjsb_ctx* ctx, const tfjsb_layer_desc* layers, 
         }
         if (step.kind == STEP_GEMM_TF32) {
             // weights [K,N] -> [N,K] once, on the device
-            if ((st = dev_alloc(m, (size_t)(step.K * step.N), &step.filter_km)) != TFJSB_OK) return bail(st, ctx->last_error);
+            if ((st = dev_alloc(m, (size_t)(step.K * step.N), &step.filter_km)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
             cudaError_t e = launch_transpose(step.filter, step.filter_km, step.K, step.N, 0, &ctx->launches);
             if (e != cudaSuccess) return bail(TFJSB_ERR_CUDA, std::string("transposing weights: ") + cudaGetErrorString(e));
         }
@@ -779,7 +779,7 @@ tfjsb_status tfjsb_model_create(tfjsb_ctx* ctx, const tfjsb_layer_desc* layers, 
             if (sp.kind == STEP_CONV_NARROW && sp.in_f32 && sp.out_bf16 && !sp.is_dense && sp.g.Co % 8 == 0 &&
                 conv_small_window_supported(sp.g) && !getenv("TFJSB_NO_PATCH_CONV")) {
                 const int64_t k_pad = conv_igemm_k_pad(sp.g);
-                if ((st = dev_alloc(m, (size_t)(k_pad * sp.g.Co), &sp.filter_km)) != TFJSB_OK) return bail(st, ctx->last_error);
+                if ((st = dev_alloc(m, (size_t)(k_pad * sp.g.Co), &sp.filter_km)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
                 cudaError_t e = launch_pack_conv_filter(sp.filter, sp.filter_km, sp.g, 0, &ctx->launches);
                 if (e != cudaSuccess) return bail(TFJSB_ERR_CUDA, std::string("packing weights: ") + cudaGetErrorString(e));
                 sp.conv_patch = true;
@@ -815,7 +815,7 @@ tfjsb_status tfjsb_model_create(tfjsb_ctx* ctx, const tfjsb_layer_desc* layers, 
     }
     m->chain_allowed = m->chain_possible = (m->use_tf32 || m->narrow) && !getenv("TFJSB_NO_FUSION");
     choose_fusion(m, m);
-    if ((st = dev_alloc(m, 2 * m->region_elems, &m->arena)) != TFJSB_OK) return bail(st, ctx->last_error);
+    if ((st = dev_alloc(m, 2 * m->region_elems, &m->arena)) != TFJSB_OK) return bail(st, tfjsb_last_error(ctx));
     cudaError_t e = cudaDeviceSynchronize();  // weight transposes done
     if (e != cudaSuccess) return bail(TFJSB_ERR_CUDA, std::string("model set-up: ") + cudaGetErrorString(e));
     ++ctx->live_models;

@@ -245,7 +245,7 @@ cudaError_t launch_clusters(void (*kernel)(KArgs...), dim3 grid, int cluster, si
     cfg.attrs = attr;
     cfg.numAttrs = n;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
-    if (e == cudaSuccess) ++*launches;
+    if (e == cudaSuccess) count_launch(launches);
     return e;
 }
 

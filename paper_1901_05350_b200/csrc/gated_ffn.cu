@@ -205,7 +205,7 @@ tfjsb_status run_layout(tfjsb_ctx* ctx, const LayoutArgs& l, bool f32, cudaStrea
     const cudaError_t e = f32 ? launch_k_serial(layout_kernel<true>, dim3((unsigned)l.blocks), dim3(256), 0, s, l)
                               : launch_k_serial(layout_kernel<false>, dim3((unsigned)l.blocks), dim3(256), 0, s, l);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "operand layout launch");
-    ++ctx->launches;
+    count_launch(&ctx->launches);
     return TFJSB_OK;
 }
 

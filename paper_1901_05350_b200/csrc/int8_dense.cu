@@ -139,7 +139,7 @@ cudaError_t launch_quantize_as(const void* x, int64_t rows, int64_t columns, int
 }
 cudaError_t launch_quantize(bool f32, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, cudaStream_t s, int64_t* launches) {
     const cudaError_t e = f32 ? launch_quantize_as<true>(x, rows, columns, q, scale, s) : launch_quantize_as<false>(x, rows, columns, q, scale, s);
-    if (e == cudaSuccess) ++*launches;
+    if (e == cudaSuccess) count_launch(launches);
     return e;
 }
 

@@ -1,0 +1,101 @@
+"""More of the dense layers of transformer blocks on the GPU: what they promise beside their values, and kernels by name."""
+import ctypes
+import math
+import threading
+
+import pytest
+import torch
+
+import dense_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.bfloat16, torch.float32]
+ids = lambda v: str(v).replace("torch.", "") if isinstance(v, torch.dtype) else None  # noqa: E731
+
+
+def normal(seed, shape, std=1.0, dtype=torch.float32):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, generator=gen, device="cuda") * std).to(dtype)
+
+
+def block(seed, t, d, f, o, dtype):
+    return (normal(seed, (t, d), 1.0, dtype), normal(seed + 1, (d, f), d ** -0.5, dtype), normal(seed + 2, (d, f), d ** -0.5, dtype),
+            normal(seed + 3, (f, o), f ** -0.5, dtype), normal(seed + 4, (t, o), 1.0, dtype))
+
+
+def at_once(*work):
+    """Each of `work` on a thread and a stream of its own; what they return."""
+    results, errors = [None] * len(work), []
+    start = threading.Barrier(len(work))
+
+    def run(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()) as _:
+                start.wait()
+                results[i] = work[i]()
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(len(work))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    return results
+
+
+# ---- several threads and streams ------------------------------------------------------------------------------------
+
+
+def test_launches_of_several_threads_are_counted(ctx):
+    x, wg, wu, wd, dy = block(1, 40, 72, 136, 72, torch.bfloat16)
+    q, s = ctx.quantize_int8(normal(6, (40, 72)))
+
+    def step():
+        y, h, z = ctx.gated_ffn(x, wg, wu, wd, save=True)
+        return (*ctx.gated_ffn_backprop(x, wg, wu, wd, h, z, ctx.dropout(dy, 0.3, 1)), ctx.gated_ffn(x[:1], wg, wu, wd), ctx.dense_int8(x, q, s), y)
+
+    before = ctx.launch_count
+    want = step()
+    each = ctx.launch_count - before
+    before = ctx.launch_count
+    got = at_once(*[lambda: [step() for _ in range(100)]] * 4)
+    assert ctx.launch_count - before == 400 * each
+    for steps in got:
+        assert all(torch.equal(a, b) for one in steps for a, b in zip(one, want))
+    ctx.check_device_status()
+
+
+def test_different_layers_side_by_side(ctx):
+    """Clusters, pairs and single CTAs of different products share the SMs."""
+    cases = [block(10 + i, *shape, dtype) for i, (shape, dtype) in enumerate((
+        ((600, 520, 1032, 520), torch.bfloat16), ((37, 2000, 456, 100), torch.bfloat16), ((300, 264, 520, 264), torch.float32)))]
+
+    def train(case):
+        x, wg, wu, wd, dy = case
+        y, h, z = ctx.gated_ffn(x, wg, wu, wd, save=True)
+        return (y, *ctx.gated_ffn_backprop(x, wg, wu, wd, h, z, dy))
+
+    want = [train(c) for c in cases]
+    got = at_once(*[lambda c=c: [train(c) for _ in range(20)] for c in cases])
+    for runs, expected in zip(got, want):
+        assert all(torch.equal(a, b) for run in runs for a, b in zip(run, expected))
+    ctx.check_device_status()
+
+
+def test_messages_of_calls_that_fail_at_once(ctx, tfjsb):
+    x, w, d = (torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in ((4, 16), (16, 32), (32, 16)))
+
+    def failing(call, text):
+        def run():
+            for _ in range(2000):
+                with pytest.raises(tfjsb.TfjsbError, match=text):
+                    call()
+        return run
+
+    at_once(failing(lambda: ctx.gated_ffn(x, w, w, d, out=x), "overlaps x"), failing(lambda: ctx.dropout(x, 1.5, 1), "rate must be"),
+            failing(lambda: ctx.dropout(x, 0.5, 1, noise_shape=(3, 16)), "each dimension of the mask"))
