@@ -15,7 +15,8 @@ namespace dense {
 //   sigmoid    s(g)
 //   relu       max(g, 0)           NaN stays NaN; slope 0 at 0
 // EXACT: for fp32 results, with functions that are good to an ulp or two; the others go into bfloat16, to which the fast
-// exponential's 2^-21 is nothing.
+// exponential's 2^-21 is nothing.  Slopes take 1 - s(v) = s(-v) from the same exponential: subtracted from 1, what is left of a large
+// v is s's rounding (at v = 12 1 % of it, at 17 all).
 template <bool EXACT>
 __device__ __forceinline__ float logistic(float v) {
     if (EXACT) {
@@ -26,16 +27,36 @@ __device__ __forceinline__ float logistic(float v) {
     return __fdividef(1.f, 1.f + __expf(-v));  // e^-v = inf: 0
 }
 
+// s(v) and s(-v), both to their own last bits
+template <bool EXACT>
+__device__ __forceinline__ void logistics(float v, float& s, float& other) {
+    float e, r;
+    if (EXACT) {
+        e = expf(-fabsf(v));
+        asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    } else {
+        e = __expf(-fabsf(v));
+        r = __fdividef(1.f, 1.f + e);
+    }
+    const float small = e * r;
+    s = v < 0.f ? small : r;  // a NaN stays one
+    other = v < 0.f ? r : small;
+}
+
 // a = gate(g) and, with SLOPE, its derivative
 template <int GATE, bool EXACT, bool SLOPE>
 __device__ __forceinline__ void gate_of(float g, float& a, float& slope) {
     if (GATE == TFJSB_GATE_SILU) {
-        const float s = logistic<EXACT>(g);
+        float s, other = 0.f;
+        if (SLOPE) logistics<EXACT>(g, s, other);
+        else s = logistic<EXACT>(g);
         a = g * s;
-        if (SLOPE) slope = s * (1.f + g * (1.f - s));
+        if (SLOPE) slope = s * (1.f + g * other);
     } else if (GATE == TFJSB_GATE_SIGMOID) {
-        a = logistic<EXACT>(g);
-        if (SLOPE) slope = a * (1.f - a);
+        float other = 0.f;
+        if (SLOPE) logistics<EXACT>(g, a, other);
+        else a = logistic<EXACT>(g);
+        if (SLOPE) slope = a * other;
     } else if (GATE == TFJSB_GATE_RELU) {
         a = relu_nan(g);
         if (SLOPE) slope = g > 0.f ? 1.f : 0.f;
@@ -55,10 +76,13 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& slope) {
         a = g * f;
         if (SLOPE) slope = fmaf(g * 0.39894228040143268f, e, f);
     } else {
-        const float g2 = fminf(g * g, 1e30f);  // finite, so that 1 - s = 0 makes the slope of large g what it is
-        const float s = logistic<EXACT>(1.5957691216057308f * g * fmaf(0.044715f, g2, 1.f));
+        const float g2 = fminf(g * g, 1e30f);  // finite, so that s(-v) = 0 makes the slope of large g what it is
+        const float v = 1.5957691216057308f * g * fmaf(0.044715f, g2, 1.f);
+        float s, other = 0.f;
+        if (SLOPE) logistics<EXACT>(v, s, other);
+        else s = logistic<EXACT>(v);
         a = g * s;
-        if (SLOPE) slope = s + a * (1.f - s) * 1.5957691216057308f * fmaf(0.134145f, g2, 1.f);
+        if (SLOPE) slope = s + a * other * 1.5957691216057308f * fmaf(0.134145f, g2, 1.f);
     }
 }
 

@@ -99,3 +99,50 @@ def test_messages_of_calls_that_fail_at_once(ctx, tfjsb):
 
     at_once(failing(lambda: ctx.gated_ffn(x, w, w, d, out=x), "overlaps x"), failing(lambda: ctx.dropout(x, 1.5, 1), "rate must be"),
             failing(lambda: ctx.dropout(x, 0.5, 1, noise_shape=(3, 16)), "each dimension of the mask"))
+
+
+# ---- slopes of the gates, value by value ----------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("gate", ["silu", "gelu", "gelu_tanh", "sigmoid", "relu"])
+def test_slopes_of_the_gates_far_out(ctx, gate, dtype):
+    """One token whose x, u and gradient of h are 1 and whose g are the weights themselves: the gradient of w_gate is the slope, that of w_up the gate.
+
+    g and what multiplies the slope are exact, so what is off is the functions': their arguments' rounding (half a step of v, which moves e^v by as
+    much of itself, a few times; g^2 / 2 in place of v for the normal distribution) and a dozen operations, each half a step or an ulp of
+    the terms that make the slope up.  bfloat16 rounds the gradient of g once more, and its exponential is off by 2 + 1.2 |v| ulps."""
+    if dtype == torch.bfloat16 and gate == "gelu":
+        pytest.skip("the gelu of bfloat16 results is good to 1e-7, not to a part of itself")
+    reach = 8 if gate.startswith("gelu") else 40
+    g = torch.arange(-reach * 16, reach * 16 + 1, device="cuda", dtype=torch.float64) / 16
+    g = g.to(dtype).double().unique()  # 1/16 is finer than bfloat16 far out
+    one = lambda *s: torch.ones(s, device="cuda", dtype=dtype)  # noqa: E731
+    n = g.numel()
+    x, wg, wu, wd = one(1, 1), g.to(dtype)[None].contiguous(), one(1, n), one(n, 1)
+    _, h, z = ctx.gated_ffn(x, wg, wu, wd, gate=gate, save=True)
+    _, slope, value, _ = ctx.gated_ffn_backprop(x, wg, wu, wd, h, z, one(1, 1), gate=gate)
+    ctx.check_device_status()
+    a, want = ref.gate(gate, g)
+    s = torch.special.expit
+    if gate == "gelu":
+        density = torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+        v, terms = g * g, torch.special.ndtr(g) + g.abs() * density
+    elif gate == "gelu_tanh":
+        v = math.sqrt(8 / math.pi) * (g + 0.044715 * g ** 3)
+        a = g * s(v)  # tanh(v) + 1 has lost its bits far out
+        factor = math.sqrt(8 / math.pi) * (1 + 3 * 0.044715 * g ** 2)
+        want = s(v) + a * s(-v) * factor
+        terms = s(v) + a.abs() * s(-v) * factor
+    else:
+        v = g
+        terms = s(g) * (1 + g.abs() * s(-g)) if gate == "silu" else s(g) * s(-g) if gate == "sigmoid" else want
+    off = (24 + 8 * v.abs()) * ref.FP32
+    if dtype == torch.bfloat16:
+        off = (64 + 16 * v.abs()) * ref.FP32
+        bounds = off * terms + ref.BF16 * (want.abs() + off * terms), off * a.abs() + ref.BF16 * a.abs() * (1 + off)
+    else:
+        bounds = off * terms, off * a.abs()
+    for got, right, bound, what in ((slope[0], want, bounds[0], "slope"), (value[0], a, bounds[1], "gate")):
+        worst = ((got.double() - right).abs() - bound).argmax()
+        assert ((got.double() - right).abs() <= bound).all(), (what, g[worst].item(), got[worst].item(), right[worst].item())
