@@ -146,3 +146,36 @@ def test_slopes_of_the_gates_far_out(ctx, gate, dtype):
     for got, right, bound, what in ((slope[0], want, bounds[0], "slope"), (value[0], a, bounds[1], "gate")):
         worst = ((got.double() - right).abs() - bound).argmax()
         assert ((got.double() - right).abs() <= bound).all(), (what, g[worst].item(), got[worst].item(), right[worst].item())
+
+
+# ---- with and without what the gradient needs -----------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("tokens", [1, 2])
+def test_a_token_or_two_without_a_gradient_are_rounded_once(ctx, tokens):
+    """Sums of one term: g = x w_gate and u = x w_up are exact, gate(g) u and the product with w_down half a step of fp32 off each at most.  Then the call that
+    keeps nothing rounds y to bfloat16, and the one that keeps h rounds h too."""
+    columns = 4096
+    x, wg, wu = normal(1, (tokens, 1), 1.0, torch.bfloat16), torch.ones(1, 1, dtype=torch.bfloat16, device="cuda"), normal(3, (1, 1), 1.0, torch.bfloat16)
+    x = x.abs()  # on relu's linear side
+    wd = normal(4, (1, columns), 1.0, torch.bfloat16)
+    want = ref.gated_ffn(x, wg, wu, wd, "relu")
+    few = ctx.gated_ffn(x, wg, wu, wd, gate="relu")
+    kept, h, z = ctx.gated_ffn(x, wg, wu, wd, gate="relu", save=True)
+    fp32 = 3 * ref.FP32
+    assert ((few.double() - want).abs() <= (ref.BF16 + fp32) * want.abs()).all()
+    assert ((kept.double() - want).abs() <= (2 * ref.BF16 + ref.BF16 ** 2 + 2 * fp32) * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_few_tokens_with_and_without_a_gradient(ctx, dtype):
+    """The two forms against each other, and against the tokens' rows among more."""
+    x, wg, wu, wd, dy = block(30, 12, 300, 520, 130, dtype)
+    bound = ref.gated_ffn_bounds(x, wg, wu, wd, dy, "gelu")[0]
+    all_of_them = ctx.gated_ffn(x, wg, wu, wd, gate="gelu")
+    for tokens in range(1, 10):
+        few, b = x[:tokens].contiguous(), bound[:tokens]
+        alone, kept = ctx.gated_ffn(few, wg, wu, wd, gate="gelu").double(), ctx.gated_ffn(few, wg, wu, wd, gate="gelu", save=True)[0].double()
+        assert ((alone - kept).abs() <= 2 * b).all() and ((alone - all_of_them[:tokens].double()).abs() <= 2 * b).all()
+        if tokens > (8 if dtype == torch.float32 else 2):  # one form for both
+            assert torch.equal(alone, kept)
