@@ -604,8 +604,15 @@ class Context:
         return q, scale
 
     def _int8_rest(self, M, N, bt_scale, bias, out_dtype, out):
-        """Checks what both 8-bit products take; (out, its tfjsb_dtype)."""
+        """Checks what both 8-bit products take; (out, its tfjsb_dtype).  `out_dtype`: as the caller gave it, or where there is no `out`
+        the default."""
         import torch
+
+        if out is not None:
+            if not isinstance(out, torch.Tensor):
+                raise TypeError("out must be a tensor")
+            if out_dtype is not None and out.dtype != out_dtype:
+                raise TypeError(f"out is {out.dtype}, out_dtype says {out_dtype}")
 
         _plain(bt_scale, "bt_scale", torch.float32, (N,), self.device)
         if bias is not None:
@@ -615,7 +622,7 @@ class Context:
 
     def matmul_int8(self, a, a_scale, bt, bt_scale, bias=None, act="none", out_dtype=None, out=None):
         """act((a . bt^T) * a_scale[:, None] * bt_scale + bias): a [M,K] and bt [N,K] int8 with K a multiple of 16 (quantize_int8 fills
-        rows up), scales and bias fp32; exact 32-bit sums; the result bfloat16 (default) or fp32."""
+        rows up), scales and bias fp32; exact 32-bit sums; the result bfloat16 (default) or fp32, or of `out`'s dtype."""
         import torch
 
         for t, name in ((a, "a"), (bt, "bt")):
@@ -625,7 +632,7 @@ class Context:
         _plain(a, "a", torch.int8, (M, K), self.device)
         _plain(bt, "bt", torch.int8, (N, K), self.device)
         _plain(a_scale, "a_scale", torch.float32, (M,), self.device)
-        out, dtype = self._int8_rest(M, N, bt_scale, bias, out_dtype or torch.bfloat16, out)
+        out, dtype = self._int8_rest(M, N, bt_scale, bias, torch.bfloat16 if out_dtype is None and out is None else out_dtype, out)
         self._check(lib.tfjsb_matmul_int8(self._h, _ptr(a), _ptr(a_scale), _ptr(bt), _ptr(bt_scale), _ptr(bias), ACT[act], _ptr(out), dtype, M, N, K,
                                           self._stream_here()))
         return out
@@ -633,7 +640,7 @@ class Context:
     def dense_int8(self, x, bt, bt_scale, bias=None, act="none", out_dtype=None, out=None):
         """A dense layer on 8-bit weights, act(q(x) . w + bias): x [M,K] bfloat16 or fp32, its rows quantised as quantize_int8 does; bt
         [N, K rounded up to a multiple of 16] and bt_scale [N] as quantize_int8 lays them out; bias fp32 [N] or None; the result in
-        x's dtype unless told otherwise."""
+        x's dtype, or `out`'s, unless told otherwise."""
         done = _fast.dense_int8(self._fh, self.device, x, bt, bt_scale, bias, ACT[act], out_dtype, out)
         if done is not None:
             return done
@@ -645,7 +652,7 @@ class Context:
         M, K, N = x.shape[0], x.shape[1], bt.shape[0]
         _plain(x, "x", x.dtype, (M, K), self.device)
         _plain(bt, "bt", torch.int8, (N, -(-K // 16) * 16), self.device)
-        out, to = self._int8_rest(M, N, bt_scale, bias, out_dtype or x.dtype, out)
+        out, to = self._int8_rest(M, N, bt_scale, bias, x.dtype if out_dtype is None and out is None else out_dtype, out)
         work = self._bytes(lib.tfjsb_dense_int8_workspace(M, K))
         self._check(lib.tfjsb_dense_int8(self._h, dtype, _ptr(x), _ptr(bt), _ptr(bt_scale), _ptr(bias), ACT[act], _ptr(out), to, M, N, K,
                                          work.data_ptr(), work.numel(), self._stream_here()))

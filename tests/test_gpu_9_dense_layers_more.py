@@ -179,3 +179,27 @@ def test_few_tokens_with_and_without_a_gradient(ctx, dtype):
         assert ((alone - kept).abs() <= 2 * b).all() and ((alone - all_of_them[:tokens].double()).abs() <= 2 * b).all()
         if tokens > (8 if dtype == torch.float32 else 2):  # one form for both
             assert torch.equal(alone, kept)
+
+
+# ---- arguments ------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("call", ["dense_int8", "matmul_int8"])
+def test_out_and_its_dtype_have_to_agree(ctx, call):
+    x = normal(1, (5, 48))
+    (w, sw), (a, sa) = ctx.quantize_int8(normal(2, (24, 48))), ctx.quantize_int8(x)
+    run = (lambda **k: ctx.dense_int8(x, w, sw, **k)) if call == "dense_int8" else (lambda **k: ctx.matmul_int8(a, sa, w, sw, **k))
+    assert run().dtype == (torch.float32 if call == "dense_int8" else torch.bfloat16)
+    for given in DTYPES:
+        want = run(out_dtype=given)
+        assert want.dtype == given
+        out = torch.empty_like(want)
+        assert run(out=out) is out and torch.equal(out, want)
+        assert torch.equal(run(out=torch.empty_like(want), out_dtype=given), want)
+        other = DTYPES[1 - DTYPES.index(given)]
+        before = ctx.launch_count
+        with pytest.raises(TypeError, match="out_dtype"):
+            run(out=out, out_dtype=other)
+        with pytest.raises(TypeError, match="out must be a tensor"):
+            run(out=out.tolist())
+        assert ctx.launch_count == before
