@@ -287,9 +287,9 @@ tfjsb_status tfjsb_bias_backprop(tfjsb_ctx* ctx, const tfjsb_tensor* dz, tfjsb_t
  * Products run on the tensor cores with fp32 sums: of bfloat16 values exactly, of fp32 values (as three bfloat16 parts) as exactly as
  * fp32 multiply-adds (parts of values below 2^-100 are flushed); without a gradient, a bfloat16 token or two and up to eight fp32 tokens on CUDA
  * cores, which is where their weights can be read fastest.  In bfloat16, g = x w_gate and u = x w_up stay fp32, the product gate(g) u is rounded
- * to bfloat16 once, and y once; for a token or two without a gradient gate(g) u stays fp32 too.  So y of a few tokens may differ from that
- * of the same tokens among more, or of a call that keeps h and z: by the rounding of gate(g) u in bfloat16, by the order of the sums in fp32.
- * An infinity among fp32 operands may give NaN where the exact result is infinite. */
+ * to bfloat16 once, and y once; for a token or two without a gradient gate(g) u stays fp32 too.  The order of the sums goes by the call's sizes
+ * and by whether it keeps h and z.  So y of some tokens may differ from that of the same tokens among more, or of a call that keeps h and z: by the
+ * order of sums, and for one or two bfloat16 tokens by the rounding of gate(g) u.  An infinity among fp32 operands may give NaN where the exact result is infinite. */
 typedef struct {
     int64_t tokens, width, hidden, out_width;
     int32_t dtype; /* tfjsb_dtype */

@@ -513,7 +513,7 @@ class Context:
         """y = (gate(x w_gate) * (x w_up)) w_down: x [..., width], w_gate and w_up [width, hidden], w_down [hidden, out_width], all bfloat16
         or all fp32; gate one of silu, gelu, gelu_tanh, sigmoid, relu.  With `save`, returns (y, h, z): what gated_ffn_backprop
         needs besides its inputs (opaque).  Without it one or two bfloat16 tokens keep gate(x w_gate) * (x w_up) in fp32 (it is rounded to bfloat16
-        once otherwise), and up to eight fp32 tokens are summed in another order: y may differ by that."""
+        once otherwise), and sums may be taken in another order: y may differ by that."""
         done = _fast.gated_ffn(self._fh, self.device, x, w_gate, w_up, w_down, GATE.get(gate, -1), save, out)
         if done is not None:
             return done

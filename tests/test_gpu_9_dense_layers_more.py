@@ -177,8 +177,6 @@ def test_few_tokens_with_and_without_a_gradient(ctx, dtype):
         few, b = x[:tokens].contiguous(), bound[:tokens]
         alone, kept = ctx.gated_ffn(few, wg, wu, wd, gate="gelu").double(), ctx.gated_ffn(few, wg, wu, wd, gate="gelu", save=True)[0].double()
         assert ((alone - kept).abs() <= 2 * b).all() and ((alone - all_of_them[:tokens].double()).abs() <= 2 * b).all()
-        if tokens > (8 if dtype == torch.float32 else 2):  # one form for both
-            assert torch.equal(alone, kept)
 
 
 # ---- arguments ------------------------------------------------------------------------------------------------------
