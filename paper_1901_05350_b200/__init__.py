@@ -558,7 +558,7 @@ class Context:
 
     def dropout_backprop(self, dy, rate: float, seed: int, offset: int = 0, noise_shape=None, out=None):
         """The gradient of x, with the same mask made again: dropout of dy without a residual."""
-        done = _fast.dropout(self._fh, self.device, dy, rate, seed, offset, noise_shape, None, out)
+        done = _fast.dropout_backprop(self._fh, self.device, dy, rate, seed, offset, noise_shape, out)
         if done is not None:
             return done
         return self._dropout(True, dy, rate, seed, offset, noise_shape, None, out)

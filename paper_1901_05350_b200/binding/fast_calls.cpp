@@ -25,7 +25,7 @@ namespace {
     X(tfjsb_binary) X(tfjsb_softmax) X(tfjsb_bias_act) X(tfjsb_conv2d_backprop_input) X(tfjsb_conv2d_backprop_filter)         \
     X(tfjsb_depthwise_conv2d_backprop_input) X(tfjsb_depthwise_conv2d_backprop_filter) X(tfjsb_act_backprop)                  \
     X(tfjsb_bias_backprop) X(tfjsb_run_model) X(tfjsb_model_layer_output_f32) X(tfjsb_model_layer_shape) X(tfjsb_window_out_shape)       \
-    X(tfjsb_last_error) X(tfjsb_gated_ffn_sizes) X(tfjsb_gated_ffn) X(tfjsb_gated_ffn_backprop) X(tfjsb_dropout) X(tfjsb_dense_int8_workspace) X(tfjsb_dense_int8)
+    X(tfjsb_last_error) X(tfjsb_gated_ffn_sizes) X(tfjsb_gated_ffn) X(tfjsb_gated_ffn_backprop) X(tfjsb_dropout) X(tfjsb_dropout_backprop) X(tfjsb_dense_int8_workspace) X(tfjsb_dense_int8)
 #define DECLARE(name) decltype(&::name) p_##name = nullptr;
 FAST_CALLS(DECLARE)
 #undef DECLARE
@@ -520,8 +520,9 @@ PyObject* gated_ffn_backprop(Args& a) {
     return all;
 }
 
-// dropout(ctx, device, x, rate, seed, offset, noise shape or None, residual or None, out)
-PyObject* dropout(Args& a) {
+// dropout(ctx, device, x, rate, seed, offset, noise shape or None, residual or None, out); of the gradient without the residual
+template <bool BACKPROP>
+PyObject* dropout_of(Args& a) {
     const Head h(a);
     int dtype = -1;
     const at::Tensor* x = dense_tensor(a, h.device, &dtype);
@@ -540,7 +541,8 @@ PyObject* dropout(Args& a) {
     else if (a.integers(noise, (int)x->dim()) != x->dim()) Py_RETURN_NONE;
     if (!a.ok) Py_RETURN_NONE;
     const at::Tensor* residual = nullptr;
-    if (*a.at == Py_None) ++a.at;
+    if (BACKPROP) {}
+    else if (*a.at == Py_None) ++a.at;
     else if (!(residual = dense_tensor(a, h.device, &dtype)) || residual->sizes() != x->sizes()) Py_RETURN_NONE;
     DenseOut out;
     out.take(a, h.device, x->sizes(), &dtype);
@@ -548,10 +550,16 @@ PyObject* dropout(Args& a) {
     void* s = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)h.device).stream();
     const double r = PyFloat_AS_DOUBLE(rate);
     return out.done(h.ctx, unlocked([&] {
+        if (BACKPROP)
+            return p_tfjsb_dropout_backprop(h.ctx, (tfjsb_dtype)dtype, x->const_data_ptr(), out.data, (int32_t)x->dim(), x->sizes().data(),
+                                            shared ? noise : nullptr, r, word[0], word[1], s);
         return p_tfjsb_dropout(h.ctx, (tfjsb_dtype)dtype, x->const_data_ptr(), residual ? residual->const_data_ptr() : nullptr, out.data, (int32_t)x->dim(),
                                x->sizes().data(), shared ? noise : nullptr, r, word[0], word[1], s);
     }));
 }
+
+PyObject* dropout(Args& a) { return dropout_of<false>(a); }
+PyObject* dropout_backprop(Args& a) { return dropout_of<true>(a); }
 
 // dense_int8(ctx, device, x, bt, bt_scale, bias or None, act, out dtype (None: x's), out)
 PyObject* dense_int8(Args& a) {
@@ -608,6 +616,7 @@ PyMethodDef methods[] = {
     METHOD("gated_ffn", gated_ffn, 9),
     METHOD("gated_ffn_backprop", gated_ffn_backprop, 10),
     METHOD("dropout", dropout, 9),
+    METHOD("dropout_backprop", dropout_backprop, 8),
     METHOD("dense_int8", dense_int8, 9),
     {nullptr, nullptr, 0, nullptr},
 };

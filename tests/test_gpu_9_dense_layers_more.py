@@ -201,3 +201,15 @@ def test_out_and_its_dtype_have_to_agree(ctx, call):
         with pytest.raises(TypeError, match="out must be a tensor"):
             run(out=out.tolist())
         assert ctx.launch_count == before
+
+
+def test_errors_of_dropouts_gradient_name_its_arguments(ctx, tfjsb):
+    dy = normal(1, (6, 10))
+    buf = torch.zeros(80, device="cuda")
+    for call, names in ((ctx.dropout, ("x", "out")), (ctx.dropout_backprop, ("dy", "dx"))):
+        with pytest.raises(tfjsb.TfjsbError, match=f"that of {names[0]} or 1"):
+            call(dy, 0.5, 1, noise_shape=(6, 2))
+        with pytest.raises(tfjsb.TfjsbError, match=f"{names[1]} overlaps an input"):
+            call(buf[:60], 0.5, 1, out=buf[4:64])
+    assert torch.equal(ctx.dropout_backprop(dy, 0.5, 1, offset=7), ctx.dropout(dy, 0.5, 1, offset=7))
+    assert torch.equal(ctx.dropout_backprop(dy, 0.5, 1, noise_shape=(6, 1), out=torch.empty_like(dy)), ctx.dropout(dy, 0.5, 1, noise_shape=(6, 1)))
