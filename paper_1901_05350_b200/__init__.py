@@ -575,8 +575,9 @@ class Context:
         if noise_shape is not None and len(noise_shape) != x.dim():
             raise ValueError("noise_shape must have x's rank")
         for v, name in ((seed, "seed"), (offset, "offset")):
-            if int(v) != v or not 0 <= v < 2 ** 64:
+            if not 0 <= v < 2 ** 64 or int(v) != v:  # in this order: int(inf) raises something else
                 raise ValueError(f"{name} must be a whole number from 0 to 2^64 - 1")
+        seed, offset = int(seed), int(offset)
         if not 1 <= x.dim() <= 4:
             raise ValueError("expected a tensor of rank 1..4")
         out = self._new(x.shape, x.dtype) if out is None else _plain(out, "out", x.dtype, x.shape, self.device)

@@ -213,3 +213,19 @@ def test_errors_of_dropouts_gradient_name_its_arguments(ctx, tfjsb):
             call(buf[:60], 0.5, 1, out=buf[4:64])
     assert torch.equal(ctx.dropout_backprop(dy, 0.5, 1, offset=7), ctx.dropout(dy, 0.5, 1, offset=7))
     assert torch.equal(ctx.dropout_backprop(dy, 0.5, 1, noise_shape=(6, 1), out=torch.empty_like(dy)), ctx.dropout(dy, 0.5, 1, noise_shape=(6, 1)))
+
+
+def test_seeds_are_whole_numbers_of_any_kind(ctx):
+    import numpy as np
+
+    x = normal(1, (300,))
+    want = ctx.dropout(x, 0.5, 3, offset=4)
+    for seed, offset in ((3.0, 4), (3, 4.0), (np.int64(3), np.uint8(4)), (np.float32(3), 4), (torch.tensor(3), 4)):
+        assert torch.equal(ctx.dropout(x, 0.5, seed, offset=offset), want)
+        assert torch.equal(ctx.dropout_backprop(x, 0.5, seed, offset=offset), want)
+    assert torch.equal(ctx.dropout(x, 0, True), x)
+    for bad in (math.inf, -math.inf, math.nan, 1e30, 0.5, -1, 2 ** 64):
+        with pytest.raises(ValueError, match="seed must be"):
+            ctx.dropout(x, 0.5, bad)
+        with pytest.raises(ValueError, match="offset must be"):
+            ctx.dropout_backprop(x, 0.5, 1, offset=bad)
