@@ -222,6 +222,17 @@ def _plain(t, name: str, dtype, shape, device: int):
     return t
 
 
+def _word(v, name: str) -> int:
+    """A whole number of 64 bits, given as an int or as anything that equals one (a float, a number of numpy's, a tensor of one element)."""
+    try:
+        word = int(v)
+    except (OverflowError, ValueError):  # an infinity, a NaN
+        word = -1
+    if word != v or not 0 <= word < 2 ** 64:
+        raise ValueError(f"{name} must be a whole number from 0 to 2^64 - 1")
+    return word
+
+
 def _ptr(t):
     return None if t is None or t.numel() == 0 else t.data_ptr()
 
@@ -574,10 +585,7 @@ class Context:
             _plain(residual, "residual", x.dtype, x.shape, self.device)
         if noise_shape is not None and len(noise_shape) != x.dim():
             raise ValueError("noise_shape must have x's rank")
-        for v, name in ((seed, "seed"), (offset, "offset")):
-            if not 0 <= v < 2 ** 64 or int(v) != v:  # in this order: int(inf) raises something else
-                raise ValueError(f"{name} must be a whole number from 0 to 2^64 - 1")
-        seed, offset = int(seed), int(offset)
+        seed, offset = _word(seed, "seed"), _word(offset, "offset")
         if not 1 <= x.dim() <= 4:
             raise ValueError("expected a tensor of rank 1..4")
         out = self._new(x.shape, x.dtype) if out is None else _plain(out, "out", x.dtype, x.shape, self.device)

@@ -126,8 +126,10 @@ def test_slopes_of_the_gates_far_out(ctx, gate, dtype):
     a, want = ref.gate(gate, g)
     s = torch.special.expit
     if gate == "gelu":
-        density = torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
-        v, terms = g * g, torch.special.ndtr(g) + g.abs() * density
+        density, f = torch.exp(-g * g / 2) / math.sqrt(2 * math.pi), torch.special.erfc(-g / math.sqrt(2)) / 2
+        # torch's ndtr is (1 + erf) / 2, which is good to 1e-16 and not to a part of itself: 1 % off at g = -7.8
+        a, want = g * f, f + g * density
+        v, terms = g * g, f + g.abs() * density
     elif gate == "gelu_tanh":
         v = math.sqrt(8 / math.pi) * (g + 0.044715 * g ** 3)
         a = g * s(v)  # tanh(v) + 1 has lost its bits far out
@@ -144,8 +146,9 @@ def test_slopes_of_the_gates_far_out(ctx, gate, dtype):
     else:
         bounds = off * terms, off * a.abs()
     for got, right, bound, what in ((slope[0], want, bounds[0], "slope"), (value[0], a, bounds[1], "gate")):
-        worst = ((got.double() - right).abs() - bound).argmax()
-        assert ((got.double() - right).abs() <= bound).all(), (what, g[worst].item(), got[worst].item(), right[worst].item())
+        over = (got.double() - right).abs() - bound
+        worst = over.argmax().item()
+        assert over[worst].item() <= 0, (what, g[worst].item(), got[worst].item(), right[worst].item())
 
 
 # ---- with and without what the gradient needs -----------------------------------------------------------------------
