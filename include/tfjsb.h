@@ -338,6 +338,11 @@ int64_t tfjsb_dense_int8_workspace(int64_t M, int64_t K);
 tfjsb_status tfjsb_dense_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, const int8_t* bt, const float* b_scale, const float* bias, tfjsb_act act,
                               void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* The tensor-core products of the calling thread's last tfjsb_gated_ffn, _backprop, _matmul_int8 or _dense_int8, in their order, as "<what becomes of
+ * the sums> <CTA group>,<columns of a tile>,<slices of K>,<parts of a tile's rows>" with "; " between them: gated, stored, gradient (of g and u)
+ * or scaled.  For tests and profiles.  Host buffer of `text_len` bytes, NUL-terminated, truncated if too short; empty where the call needed none. */
+tfjsb_status tfjsb_dense_kernels(tfjsb_ctx* ctx, char* text, int32_t text_len);
+
 /* ---- models ------------------------------------------------------------------------- */
 
 typedef enum {

@@ -40,6 +40,7 @@ EXPORTS = [
     "tfjsb_depthwise_conv2d_backprop_input", "tfjsb_depthwise_conv2d_backprop_filter", "tfjsb_act_backprop",
     "tfjsb_bias_backprop", "tfjsb_gated_ffn_sizes", "tfjsb_gated_ffn", "tfjsb_gated_ffn_backprop", "tfjsb_dropout",
     "tfjsb_dropout_backprop", "tfjsb_quantize_int8", "tfjsb_matmul_int8", "tfjsb_dense_int8_workspace", "tfjsb_dense_int8",
+    "tfjsb_dense_kernels",
 ]
 
 
@@ -134,6 +135,7 @@ def _load_library() -> ctypes.CDLL:
     lib.tfjsb_matmul_int8.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, i32, i64, i64, i64, vp]
     lib.tfjsb_dense_int8_workspace.argtypes = [i64, i64]
     lib.tfjsb_dense_int8_workspace.restype = i64
+    lib.tfjsb_dense_kernels.argtypes = [vp, ctypes.c_char_p, ctypes.c_int32]
     lib.tfjsb_dense_int8.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, i32, i64, i64, i64, vp, i64, vp]
     return lib
 
@@ -666,6 +668,13 @@ class Context:
         self._check(lib.tfjsb_dense_int8(self._h, dtype, _ptr(x), _ptr(bt), _ptr(bt_scale), _ptr(bias), ACT[act], _ptr(out), to, M, N, K,
                                          work.data_ptr(), work.numel(), self._stream_here()))
         return out
+
+    def dense_kernels(self):
+        """The tensor-core products of this thread's last gated_ffn, gated_ffn_backprop, matmul_int8 or dense_int8, in order: pairs of what became of the
+        sums ("gated", "stored", "gradient", "scaled") and the kernel's shape ("CTA group,columns,slices,parts", as in TFJSB_DENSE_SHAPE)."""
+        buf = ctypes.create_string_buffer(256)
+        self._check(lib.tfjsb_dense_kernels(self._h, buf, len(buf)))
+        return [tuple(p.split(" ")) for p in buf.value.decode().split("; ") if p]
 
     def model(self, layers: Sequence, input_shape) -> "Model":
         return Model(self, layers, input_shape)

@@ -59,6 +59,12 @@ struct Product {
     Args args;
 };
 tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s);
+// The kernels of the calling thread's products since its call began (tfjsb_dense_kernels).
+struct Ran {
+    struct { Epilogue epilogue; int cg, block_n, splits, subs; } product[8];
+    int count = 0;
+};
+Ran& ran();
 
 // Products of few rows (few_rows.cu).  h is fp32 [rows, N]; operands 16-byte aligned, of any sizes.  FEW_ROWS at most; where the tensor
 // cores take the weights as they are stored (bfloat16) they are faster from three rows on (1024 x 4096: 2 rows 12 against 16 us, 4 rows 20 against

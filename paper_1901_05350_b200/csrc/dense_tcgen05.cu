@@ -31,6 +31,7 @@
 // additions: the large products go to an accumulator of their own for `seg_kb` k-blocks only (8 additions), the small ones
 // to another, and the epilogue adds both to fp32 sums in registers, rounded to nearest.
 #include <atomic>
+#include <cstdio>
 #include <cstdlib>
 
 #include <cuda_bf16.h>
@@ -1111,6 +1112,11 @@ Shape choose(const Product& p, int dev, int sm_count) {
 
 }  // namespace
 
+Ran& ran() {
+    static thread_local Ran r;
+    return r;
+}
+
 tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
     if (!ctx->encode_tiled) return fail(ctx, TFJSB_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
     Args& a = p.args;
@@ -1167,8 +1173,27 @@ tfjsb_status run_product(tfjsb_ctx* ctx, Product& p, cudaStream_t s) {
                           : c.cg == 2                  ? launch_any<2, 3, 1>(p, maps, grid, smem, s, &ctx->launches)
                           : p.planes == 1              ? launch_any<1, 1, 1>(p, maps, grid, smem, s, &ctx->launches)
                                                        : launch_any<1, 3, 1>(p, maps, grid, smem, s, &ctx->launches);
-    return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "dense product launch");
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "dense product launch");
+    Ran& r = ran();
+    if (r.count < 8) r.product[r.count++] = {p.epilogue, c.cg, c.block_n, c.splits, c.subs};
+    return TFJSB_OK;
 }
 
 }  // namespace dense
 }  // namespace tfjsb
+
+extern "C" tfjsb_status tfjsb_dense_kernels(tfjsb_ctx* ctx, char* text, int32_t text_len) {
+    using namespace tfjsb;
+    if (!ctx) return TFJSB_ERR_INVALID_ARG;
+    if (!text || text_len < 1) return fail(ctx, TFJSB_ERR_INVALID_ARG, "text is null or has no room");
+    const dense::Ran& r = dense::ran();
+    std::string all;
+    for (int i = 0; i < r.count; ++i) {
+        const auto& k = r.product[i];
+        const char* name = k.epilogue == dense::EPI_STORE ? "stored" : k.epilogue == dense::EPI_GATED ? "gated" : k.epilogue == dense::EPI_GRAD ? "gradient" : "scaled";
+        all += std::string(i ? "; " : "") + name + " " + std::to_string(k.cg) + "," + std::to_string(k.block_n) + "," + std::to_string(k.splits) + "," +
+               std::to_string(k.subs);
+    }
+    snprintf(text, (size_t)text_len, "%s", all.c_str());
+    return TFJSB_OK;
+}

@@ -267,6 +267,7 @@ tfjsb_status tfjsb_gated_ffn(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, const void* x
                              void* h, void* z, void* workspace, int64_t workspace_bytes, void* stream) {
     if (!ctx) return TFJSB_ERR_INVALID_ARG;
     const dense::OnDevice on(ctx);
+    ran().count = 0;
     Sizes s;
     std::string why;
     tfjsb_status st = sizes_of(ffn, &s, &why);
@@ -326,6 +327,7 @@ tfjsb_status tfjsb_gated_ffn_backprop(tfjsb_ctx* ctx, const tfjsb_ffn* ffn, cons
                                       void* workspace, int64_t workspace_bytes, void* stream) {
     if (!ctx) return TFJSB_ERR_INVALID_ARG;
     const dense::OnDevice on(ctx);
+    ran().count = 0;
     Sizes s;
     std::string why;
     tfjsb_status st = sizes_of(ffn, &s, &why);

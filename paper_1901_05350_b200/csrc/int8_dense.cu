@@ -224,6 +224,7 @@ tfjsb_status tfjsb_matmul_int8(tfjsb_ctx* ctx, const int8_t* a, const float* a_s
                                tfjsb_act act, void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, void* stream) {
     if (!ctx) return TFJSB_ERR_INVALID_ARG;
     const dense::OnDevice on(ctx);
+    ran().count = 0;
     const tfjsb_status st = check_product(ctx, bt, b_scale, bias, act, out, out_dtype, M, N, K);
     if (st != TFJSB_OK) return st;
     if (K % 16) return fail(ctx, TFJSB_ERR_UNSUPPORTED, "K must be a multiple of 16: fill rows up with zeros");
@@ -244,6 +245,7 @@ tfjsb_status tfjsb_dense_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, 
                               void* out, tfjsb_dtype out_dtype, int64_t M, int64_t N, int64_t K, void* workspace, int64_t workspace_bytes, void* stream) {
     if (!ctx) return TFJSB_ERR_INVALID_ARG;
     const dense::OnDevice on(ctx);
+    ran().count = 0;
     if (!known(dtype)) return fail(ctx, TFJSB_ERR_INVALID_ARG, "unknown dtype");
     const tfjsb_status st = check_product(ctx, bt, b_scale, bias, act, out, out_dtype, M, N, K);
     if (st != TFJSB_OK) return st;

@@ -232,3 +232,95 @@ def test_seeds_are_whole_numbers_of_any_kind(ctx):
             ctx.dropout(x, 0.5, bad)
         with pytest.raises(ValueError, match="offset must be"):
             ctx.dropout_backprop(x, 0.5, 1, offset=bad)
+
+
+# ---- kernels by name ------------------------------------------------------------------------------------------------
+
+
+def kernels(ctx, what):
+    return [shape for name, shape in ctx.dense_kernels() if name == what]
+
+
+def test_the_kernels_of_a_call_are_named(ctx, tfjsb):
+    x, wg, wu, wd, dy = block(1, 40, 72, 136, 72, torch.bfloat16)
+    y, h, z = ctx.gated_ffn(x, wg, wu, wd, save=True)
+    assert [n for n, _ in ctx.dense_kernels()] == ["gated", "stored"]
+    ctx.gated_ffn_backprop(x, wg, wu, wd, h, z, dy)
+    assert [n for n, _ in ctx.dense_kernels()] == ["gradient", "stored", "stored", "stored"]
+    ctx.gated_ffn(x[:1], wg, wu, wd)
+    assert ctx.dense_kernels() == []
+    q, s = ctx.quantize_int8(normal(1, (200, 72)))
+    ctx.dense_int8(x, q, s)
+    assert [n for n, _ in ctx.dense_kernels()] == []  # small: one kernel on CUDA cores
+    ctx.matmul_int8(*ctx.quantize_int8(x), q, s)
+    assert [n for n, _ in ctx.dense_kernels()] == ["scaled"]
+    short = ctypes.create_string_buffer(4)
+    assert tfjsb.lib.tfjsb_dense_kernels(ctx._h, short, 4) == 0 and short.value == b"sca"
+    assert tfjsb.lib.tfjsb_dense_kernels(ctx._h, None, 4) == tfjsb.lib.tfjsb_dense_kernels(None, short, 4) == 1
+
+
+def check_block(ctx, shape, dtype, seed, gate="silu"):
+    """Forward and gradients within their bounds; the kernels of both calls: (forward's, backward's)."""
+    x, wg, wu, wd, dy = block(seed, *shape, dtype)
+    y, h, z = ctx.gated_ffn(x, wg, wu, wd, gate=gate, save=True)
+    forward = ctx.dense_kernels()
+    grads = ctx.gated_ffn_backprop(x, wg, wu, wd, h, z, dy, gate=gate)
+    backward = ctx.dense_kernels()
+    ctx.check_device_status()
+    want = [ref.gated_ffn(x, wg, wu, wd, gate), *ref.gated_ffn_gradients(x, wg, wu, wd, dy, gate)]
+    for got, w, b, what in zip((y, *grads), want, ref.gated_ffn_bounds(x, wg, wu, wd, dy, gate), ("y", "dx", "dw_gate", "dw_up", "dw_down")):
+        off = (got.double() - w).abs()
+        assert got.dtype == dtype and torch.isfinite(got).all() and (off <= b).all(), (what, shape, (off - b).max().item())
+        # in the norm: two independent roundings to bfloat16, or fp32 sums cut towards zero in segments of eight additions
+        assert off.norm() <= (2.0 ** -8 if dtype == torch.bfloat16 else 2e-6) * w.norm(), (what, shape)
+    assert [n for n, _ in forward] == ["gated", "stored"] and [n for n, _ in backward] == ["gradient", "stored", "stored", "stored"]
+    return [k for _, k in forward], [k for _, k in backward]
+
+
+LONG = 2520  # 40 k-blocks, the last one not whole: two to eight slices of four k-blocks or more, none without any
+# products whose K is long: tokens, width, hidden, out width, and where they are among the six of check_block
+SLICED = {"gated": ((150, LONG, 200, 72), [0]), "stored and dx": ((150, 200, LONG, 200), [1, 4]), "gradient": ((150, 72, 200, LONG), [2]),
+          "weights": ((LONG, 100, 200, 200), [3, 5]), "few rows, gated": ((37, LONG, 200, 72), [0]), "few rows, stored": ((37, 100, LONG, 200), [1, 4]),
+          "few rows, gradient": ((37, 72, 200, LONG), [2])}
+
+
+@pytest.mark.parametrize("slices", [2, 3, 4, 5, 6, 7, 8])
+@pytest.mark.parametrize("dtype,columns", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.bfloat16, 256), (torch.float32, 128)], ids=str)
+@pytest.mark.parametrize("what", list(SLICED))
+def test_every_product_in_slices(ctx, monkeypatch, what, dtype, columns, slices):
+    shape, places = SLICED[what]
+    if columns == 64 and "gated" in what:
+        pytest.skip("a gated tile of 64 columns has 32 of each weight, half a box")
+    if columns == 256 and slices == 7 and what == "gated":
+        pytest.skip("seven slices' sums of 128 rows of g and u have 196 KiB, more than the stages that they take the place of")
+    kernel = f"1,{columns},{slices},1"
+    monkeypatch.setenv("TFJSB_DENSE_SHAPE", kernel)
+    forward, backward = check_block(ctx, shape, dtype, 500 + columns + slices)
+    assert [(forward + backward)[i] for i in places] == [kernel] * len(places)
+
+
+@pytest.mark.parametrize("kernel", ["1,64,1,1", "1,128,1,1", "1,256,1,1", "2,128,1,1", "2,256,1,1", "2,256,1,2"])
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_every_product_on_every_unsliced_kernel(ctx, monkeypatch, kernel, dtype):
+    """Fp32 products have tiles of 128 columns alone; tiles of 64 are not for the gated one."""
+    if dtype == torch.float32 and kernel.split(",")[1] != "128":
+        pytest.skip("fp32 products have 128 columns a tile")
+    monkeypatch.setenv("TFJSB_DENSE_SHAPE", kernel)
+    for shape in ((200, 600, 328, 136), (37, 1100, 513, 260)):
+        forward, backward = check_block(ctx, shape, dtype, 600)
+        assert (forward + backward)[1 if kernel.startswith("1,64") else 0:] == [kernel] * (5 if kernel.startswith("1,64") else 6)
+
+
+@pytest.mark.parametrize("columns", [64, 128, 256])
+@pytest.mark.parametrize("slices", [1, 2, 3, 4, 5, 6, 7, 8])
+def test_int8_products_in_slices(ctx, monkeypatch, columns, slices):
+    """Whole numbers: the sums have to be exact."""
+    kernel = f"1,{columns},{slices},1"
+    monkeypatch.setenv("TFJSB_DENSE_SHAPE", kernel)
+    for M, K, N in ((150, 5040, 200), (37, 5056, 130)):  # 40 k-blocks of 128
+        gen = torch.Generator(device="cuda").manual_seed(M + slices)
+        a, w = (torch.randint(-128, 128, (rows, K), generator=gen, device="cuda").to(torch.int8) for rows in (M, N))
+        y = ctx.matmul_int8(a, torch.ones(M, device="cuda"), w, torch.ones(N, device="cuda"), out_dtype=torch.float32)
+        assert kernels(ctx, "scaled") == [kernel]
+        ctx.check_device_status()
+        assert torch.equal(y, (a.double() @ w.double().T).float())
