@@ -324,3 +324,33 @@ def test_int8_products_in_slices(ctx, monkeypatch, columns, slices):
         assert kernels(ctx, "scaled") == [kernel]
         ctx.check_device_status()
         assert torch.equal(y, (a.double() @ w.double().T).float())
+
+
+# ---- several tiles a CTA --------------------------------------------------------------------------------------------
+
+# Tokens, width, hidden, out width; which of the six products have 1.4 rounds of tiles or more on CTA pairs and on single CTAs.  264 and 328 are five and six
+# k-blocks, three segments of two: a tile begins on the other accumulator than the one before it.
+ROUNDS = [((2600, 264, 2300, 328), [0, 2]), ((2600, 2100, 264, 2100), [1, 4]), ((264, 2600, 2300, 2100), [3, 5])]
+
+
+@pytest.mark.parametrize("kernel", ["1,128,1,1", "2,128,1,1"])
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("shape,places", ROUNDS, ids=str)
+def test_rounds_of_tiles(ctx, monkeypatch, shape, places, dtype, kernel):
+    """Accumulators and segments of sums in turn from tile to tile, one tile's epilogue beside the next one's sums, for every product."""
+    monkeypatch.setenv("TFJSB_DENSE_SHAPE", kernel)
+    group = int(kernel[0])
+    t, d, f, o = shape
+    tiles = lambda m, n, columns=128: -(-m // (128 * group)) * -(-n // columns)  # noqa: E731
+    # in the order of the two calls' products: gated, y; gradients of g and u, w_down, x, w_gate and w_up
+    counts = [tiles(t, f, 64), tiles(t, o), tiles(t, f), tiles(f, o), tiles(t, d), 2 * tiles(d, f)]
+    slots = torch.cuda.get_device_properties(0).multi_processor_count // group
+    assert all(counts[i] >= 1.4 * slots for i in places), counts
+    forward, backward = check_block(ctx, shape, dtype, 700, "gelu")
+    assert forward + backward == [kernel] * 6
+
+
+@pytest.mark.parametrize("shape", [(2048, 1024, 4096, 1024), (1999, 1000, 2600, 900)], ids=str)
+def test_ordinary_fp32_blocks_of_several_rounds(ctx, shape):
+    """The kernels that the call takes by itself."""
+    check_block(ctx, shape, torch.float32, 800)
