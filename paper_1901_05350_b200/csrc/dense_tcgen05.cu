@@ -107,6 +107,31 @@ __device__ __forceinline__ void sts16_cluster(uint32_t at, const uint32_t* v) {
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 
+// bounded_wait with more than one limit after the other, where the time may be somebody else's.
+//   A role that begins before the kernel before has ended (its operands are not that kernel's, or it waits for a role that does wait for
+//   that kernel) may spend a limit on it: few tiles with an enormous K keep a handful of SMs busy while the others are this kernel's
+//   already.  So that kernel is waited for, and then the limit is this kernel's own.
+//   An epilogue, which has been through that wait, waits for all of a tile's k-blocks: it has a limit for each 65536 of them (of 250 ns each where K is
+//   cut eight ways and a tile is small: 2^30 terms take 0.52 s).
+// One function and no calls from it: calls of bounded_wait_slow, or of a second function after it, made short products 1 to 2 % slower.
+__device__ __noinline__ bool patient_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, int limits) {
+#pragma unroll 1
+    for (;;) {
+        const unsigned long long t0 = global_ns();
+#pragma unroll 1
+        for (uint32_t it = 1; it < (1u << 26); ++it) {
+            if (mbar_try_wait(bar, parity)) return true;
+            if (*abort_flag) return false;
+            if ((it & 63u) == 0u && global_ns() - t0 > WAIT_LIMIT_NS) break;
+        }
+        if (--limits <= 0) return false;
+        pdl_wait();
+    }
+}
+__device__ __forceinline__ bool patient_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int limits = 2) {
+    return mbar_try_wait(bar, parity) || patient_wait_slow(bar, parity, abort_flag, limits);
+}
+
 __device__ __forceinline__ uint4 lds4u(uint32_t at) {
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
@@ -411,7 +436,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                         c1[i] = A_MN ? k0 : row;
                         c2[i] = pass * P + p;
                     }
-                    if (elected && ok && (ready || (ok = bounded_wait(empty, phase ^ 1u, abort_flag)))) {
+                    if (elected && ok && (ready || (ok = patient_wait(empty, phase ^ 1u, abort_flag)))) {
                         ready = mbar_test_wait(next_empty, next_phase ^ 1u);
                         if (leader) mbar_arrive_expect_tx(own_full, tx);
 #pragma unroll
@@ -433,7 +458,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                         c1[i] = B_MN ? k0 : row;
                         c2[i] = which * P + p;
                     }
-                    if (elected && ok && (ready || (ok = bounded_wait(empty, phase ^ 1u, abort_flag)))) {
+                    if (elected && ok && (ready || (ok = patient_wait(empty, phase ^ 1u, abort_flag)))) {
                         ready = mbar_test_wait(next_empty, next_phase ^ 1u);
 #pragma unroll
                         for (int i = 0; i < B_COPIES; ++i)
@@ -502,7 +527,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                         for (int part = 0; part < 2; ++part) {
                             if (part >= subs) break;
                             if (kb == kb_begin) {
-                                if (elected && ok) ok = bounded_wait(acc_empty_0 + 8u * part, part_phase[part] ^ 1u, abort_flag);
+                                if (elected && ok) ok = patient_wait(acc_empty_0 + 8u * part, part_phase[part] ^ 1u, abort_flag);
                                 part_phase[part] ^= 1u;
                                 tc_fence_after();
                             }
@@ -517,7 +542,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                                 const bool last = part + 1 == subs;
                                 advance();
                                 const uint32_t next_full = full_0 + 8u * stage, next_phase = phase, this_phase = phase ^ (stage == 0 ? 1u : 0u);
-                                if (elected && ok && (part > 0 || ready || (ok = bounded_wait(full, this_phase, abort_flag)))) {
+                                if (elected && ok && (part > 0 || ready || (ok = patient_wait(full, this_phase, abort_flag)))) {
                                     if (part == 0) tc_fence_after();
                                     ready = mbar_test_wait(next_full, next_phase);
                                     mma<CG, KIND>(d, a0, a_hi, b0, b_hi, idesc, begun);
@@ -540,7 +565,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                     int in_segment = 0;
                     for (int kb = kb_begin; kb < kb_end; ++kb) {
                         if (in_segment == 0 && elected && ok) {
-                            ok = bounded_wait(acc_empty_0 + 8u * acc, acc_phase ^ 1u, abort_flag);
+                            ok = patient_wait(acc_empty_0 + 8u * acc, acc_phase ^ 1u, abort_flag);
                             tc_fence_after();
                         }
                         const uint32_t d = tmem_base + (uint32_t)acc * acc_cols, small = d + (uint32_t)block_n;
@@ -555,7 +580,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
                         const uint32_t begun = in_segment != 0 ? 1u : 0u, full = full_0 + 8u * stage, empty = empty_0 + 8u * stage;
                         advance();
                         const uint32_t next_full = full_0 + 8u * stage, next_phase = phase, this_phase = phase ^ (stage == 0 ? 1u : 0u);
-                        if (elected && ok && (ready || (ok = bounded_wait(full, this_phase, abort_flag)))) {
+                        if (elected && ok && (ready || (ok = patient_wait(full, this_phase, abort_flag)))) {
                             tc_fence_after();
                             ready = mbar_test_wait(next_full, next_phase);
 #pragma unroll
@@ -615,7 +640,7 @@ dense_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args arg
         uint32_t phases = 0;  // of the accumulators, a bit each
         bool ok = true;
         auto wait_acc = [&]() {
-            const bool got = bounded_wait(smem_u32(&bar_acc_full[acc]), phases >> acc & 1u, abort_flag);
+            const bool got = patient_wait(smem_u32(&bar_acc_full[acc]), phases >> acc & 1u, abort_flag, 1 + ((kb_end - kb_begin) >> 16));
             if (!__all_sync(0xffffffffu, got)) {
                 if (lane == 0) give_up(abort_flag, args.dev_status, DEV_STATUS_TIMEOUT_EPILOGUE);
                 return false;

@@ -354,3 +354,37 @@ def test_rounds_of_tiles(ctx, monkeypatch, shape, places, dtype, kernel):
 def test_ordinary_fp32_blocks_of_several_rounds(ctx, shape):
     """The kernels that the call takes by itself."""
     check_block(ctx, shape, torch.float32, 800)
+
+
+# ---- the longest sums -----------------------------------------------------------------------------------------------
+
+
+def sparse(rows, columns, places, value):
+    """Zeros but for `value` at `places`."""
+    m = torch.zeros(rows, columns, dtype=torch.bfloat16, device="cuda")
+    for r, c in places:
+        m[r, c] = value
+    return m
+
+
+@pytest.mark.parametrize("what", ["width", "hidden"])
+def test_sums_of_2_30_terms(ctx, what):
+    """A handful of CTAs sum for half a second, the longest that a wait may take without progress: the epilogue waits for all of it, and the kernel after
+    it, which begins on the other SMs, for its end.  All terms but a few are zero, so the sums are exact."""
+    n, tokens, few = 2 ** 30, 3, 8
+    at = [0, 1, 12345, n // 8 - 1, n // 8, n // 2 + 77, n - 65, n - 1]
+    if what == "width":  # g = x w_gate
+        x = sparse(tokens, n, [(t, k) for t in range(tokens) for k in at], 1.0)
+        wg, wu = sparse(n, few, [(k, c) for k in at for c in range(few)], 1.0), sparse(n, few, [(at[-1], c) for c in range(few)], 1.0)
+        wd = sparse(few, few, [(c, c) for c in range(few)], 0.5)
+        y, want = ctx.gated_ffn(x, wg, wu, wd, gate="relu"), 0.5 * len(at)
+    else:  # y = h w_down
+        x = sparse(tokens, few, [(t, 0) for t in range(tokens)], 1.0)
+        wg, wd = sparse(few, n, [(0, k) for k in at], 2.0), sparse(n, few, [(k, c) for k in at for c in range(few)], 1.0)
+        wu = wg
+        y, want = ctx.gated_ffn(x, wg, wu, wd, gate="relu"), 4.0 * len(at)
+    ctx.check_device_status()
+    assert ctx.dense_kernels()[0 if what == "width" else 1][1].split(",")[2] == "8"
+    assert y.shape == (tokens, few) and (y == want).all(), y
+    del x, wg, wu, wd
+    torch.cuda.empty_cache()
