@@ -124,10 +124,10 @@ __global__ void __launch_bounds__(128) quantize_rows_kernel(const void* x, int64
 }
 
 template <bool F32>
-cudaError_t launch_quantize_as(const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, cudaStream_t s) {
+cudaError_t launch_quantize_as(int sm_count, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, cudaStream_t s) {
     const int64_t pitch = (columns + 15) / 16 * 16;
-    // a warp a row where that is enough warps for the GPU
-    if (rows >= 148 * 8 && columns % 8 == 0 && columns <= (F32 ? 2048 : 4096)) {
+    // a warp a row where that is enough warps for the GPU: eight an SM
+    if (rows >= (int64_t)sm_count * 8 && columns % 8 == 0 && columns <= (F32 ? 2048 : 4096)) {
         constexpr int ALL = 16;
         auto* kernel = columns <= (F32 ? 512 : 1024) ? &quantize_rows_kernel<F32, ALL / 4>
                        : columns <= (F32 ? 1024 : 2048) ? &quantize_rows_kernel<F32, ALL / 2>
@@ -137,9 +137,10 @@ cudaError_t launch_quantize_as(const void* x, int64_t rows, int64_t columns, int
     auto* kernel = columns <= 2048 ? &quantize_kernel<F32, 1> : columns <= 4096 ? &quantize_kernel<F32, 2> : &quantize_kernel<F32, 4>;
     return launch_k(kernel, dim3((unsigned)rows), dim3(QUANTIZE_THREADS), 0, s, x, columns, pitch, q, scale);
 }
-cudaError_t launch_quantize(bool f32, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, cudaStream_t s, int64_t* launches) {
-    const cudaError_t e = f32 ? launch_quantize_as<true>(x, rows, columns, q, scale, s) : launch_quantize_as<false>(x, rows, columns, q, scale, s);
-    if (e == cudaSuccess) count_launch(launches);
+cudaError_t launch_quantize(tfjsb_ctx* ctx, bool f32, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, cudaStream_t s) {
+    const cudaError_t e = f32 ? launch_quantize_as<true>(ctx->sm_count, x, rows, columns, q, scale, s)
+                              : launch_quantize_as<false>(ctx->sm_count, x, rows, columns, q, scale, s);
+    if (e == cudaSuccess) count_launch(&ctx->launches);
     return e;
 }
 
@@ -216,7 +217,7 @@ tfjsb_status tfjsb_quantize_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* 
     const int64_t in = rows * columns * (dtype == TFJSB_DTYPE_F32 ? 4 : 2), out = rows * up16(columns);
     if (overlap(x, in, q, out) || overlap(x, in, scale, 4 * rows) || overlap(q, out, scale, 4 * rows))
         return fail(ctx, TFJSB_ERR_INVALID_ARG, "x, q and scale overlap");
-    const cudaError_t e = launch_quantize(dtype == TFJSB_DTYPE_F32, x, rows, columns, q, scale, static_cast<cudaStream_t>(stream), &ctx->launches);
+    const cudaError_t e = launch_quantize(ctx, dtype == TFJSB_DTYPE_F32, x, rows, columns, q, scale, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? TFJSB_OK : cuda_fail(ctx, e, "quantize launch");
 }
 
@@ -263,7 +264,7 @@ tfjsb_status tfjsb_dense_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, 
         return rows_int8(ctx, dtype == TFJSB_DTYPE_F32 ? 2 : 1, x, nullptr, bt, b_scale, bias, act, out, out_dtype == TFJSB_DTYPE_BF16, M, N, K, s);
     int8_t* q = static_cast<int8_t*>(workspace);
     float* scale = reinterpret_cast<float*>(q + up256(M * up16(K)));
-    const cudaError_t e = launch_quantize(dtype == TFJSB_DTYPE_F32, x, M, K, q, scale, s, &ctx->launches);
+    const cudaError_t e = launch_quantize(ctx, dtype == TFJSB_DTYPE_F32, x, M, K, q, scale, s);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "quantize launch");
     return product(ctx, q, scale, bt, b_scale, bias, act, out, out_dtype, M, N, up16(K), true, s);
 }
