@@ -284,7 +284,8 @@ tfjsb_status tfjsb_bias_backprop(tfjsb_ctx* ctx, const tfjsb_tensor* dz, tfjsb_t
 /* A gated feed-forward block: y = (gate(x w_gate) * (x w_up)) w_down, no biases.
  *   x [tokens,width], w_gate and w_up [width,hidden], w_down [hidden,out_width], y [tokens,out_width], all of `dtype`.
  * Any sizes from 1 to 2^30 (tokens may be 0) whose buffers have 2^60 bytes each at most; operands whose rows are no multiple of 16 bytes are copied into the workspace first.
- * Products run on the tensor cores with fp32 sums: of bfloat16 values exactly, of fp32 values (as three bfloat16 parts) as exactly as
+ * Products run on the tensor cores with fp32 sums: of bfloat16 values exactly (each addition of 16 products cuts the sum towards zero, which shows
+ * in sums of more than 2^22 terms), of fp32 values (as three bfloat16 parts) as exactly as
  * fp32 multiply-adds (parts of values below 2^-100 are flushed); without a gradient, a bfloat16 token or two and up to eight fp32 tokens on CUDA
  * cores, which is where their weights can be read fastest.  In bfloat16, g = x w_gate and u = x w_up stay fp32, the product gate(g) u is rounded
  * to bfloat16 once, and y once; for a token or two without a gradient gate(g) u stays fp32 too.  The order of the sums goes by the call's sizes

@@ -66,9 +66,11 @@ struct Ran {
 };
 Ran& ran();
 
-// Products of few rows (few_rows.cu).  h is fp32 [rows, N]; operands 16-byte aligned, of any sizes.  FEW_ROWS at most; where the tensor
-// cores take the weights as they are stored (bfloat16) they are faster from three rows on (1024 x 4096: 2 rows 12 against 16 us, 4 rows 20 against
-// 16), where the weights would be split into planes first (fp32) they are not.
+// Products of few rows (few_rows.cu).  h is fp32 [rows, N]; operands 16-byte aligned, of any sizes.  FEW_ROWS at most.
+// bfloat16, whose weights the tensor cores take as they are stored: one or two rows.  Blocks of width x hidden, us of one row and of two, on
+// CUDA cores | on tensor cores: 1024 x 4096 (24 MB, in L2) 11, 12 | 15, 15; 2048 x 8192 (100 MB, four sets of weights in turn) 34, 36 | 28, 28;
+// 4096 x 16384 (402 MB) 83, 93 | 68, 68.  So where weights come from HBM the tensor cores are ahead already; the rule does not know that yet.
+// fp32, whose weights would be split into planes first: one, eight rows 17, 38 | 64, 62; 70, 124 | 163, 171; 225, 368 | 584, 638.
 constexpr int FEW_ROWS = 8;
 constexpr int few_rows_ffn(bool f32) { return f32 ? FEW_ROWS : 2; }
 tfjsb_status few_rows_gated(tfjsb_ctx* ctx, bool f32, const void* x, const void* w_gate, const void* w_up, int gate, float* h, int64_t rows, int64_t N,

@@ -16,7 +16,9 @@
 // every sector is written once and whole; g and u are in blocks of 32 rows x 8 columns, which a warp moves in one piece.
 //
 // What bounds it: at large sizes what an SM can fetch from L2 (50 to 60 bytes a cycle), so the widest tile is 512 x 256 for a CTA pair, two parts
-// of 256 rows that share B (SUBS = 2): 8192 x 4096 x 16384 took 1.62-1.64 PFLOP/s of the burst, with 256 x 256 tiles 1.35.  At small ones
+// of 256 rows that share B (SUBS = 2): h Wd of 8192 x 4096 x 16384 took 1.62-1.64 PFLOP/s in a burst, with 256 x 256 tiles 1.35.  Epilogues
+// with more to do take their share: x Wg and x Wu, whose gates and copies of g and u hold up the next tile, 1.45-1.48 (tensor pipe 72 % active),
+// the gradients of g and u, which read 8 bytes an element and have tiles of one part, 1.28 (64 %).  At small sizes
 // latency: a launch, the first copies (2 us) and the epilogue.
 // Persistent over tiles in bands of `band` tile rows, so that the tiles in flight share operand rows and columns in L2.
 //

@@ -51,8 +51,8 @@ __device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
 }
 
 // The four words of a block.  The offset is the same for all, so one product of the first round is worked out before the launch, and so is one of
-// the second where the upper half of the block's index is 0 (SMALL: less than 2^34 elements).  The multiplier that makes 64 bits of 32 is
-// what bounds the kernel next to memory: 18 of them a block instead of 20.
+// the second where the upper half of the block's index is 0 (SMALL: less than 2^34 elements).  The products that make 64 bits of 32
+// are what the words cost most: 18 of them a block instead of 20.
 template <bool SMALL>
 __device__ __forceinline__ void philox(const DropoutArgs& a, uint64_t block, uint32_t (&w)[4]) {
     uint32_t h0, l0, h1, l1;

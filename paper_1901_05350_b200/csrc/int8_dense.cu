@@ -145,8 +145,10 @@ cudaError_t launch_quantize(tfjsb_ctx* ctx, bool f32, const void* x, int64_t row
 }
 
 // One kernel on CUDA cores instead of two launches: a single row, and layers so small that launching takes longest.  A warp of it takes 0.2 ns of the
-// GPU's time for each output, and 0.1 ns more per 1000 values of K: where that is less than 2.6 us in all it is faster than the two
-// kernels (8 x 1024 x 1024: 6.2 us a call, two kernels 7.5; 32 x 256 x 256 5.7 and 7.5; beyond, 64 x 256 x 256, 7.9 and 7.4).
+// GPU's time for each output, and 0.1 ns more per 1000 values of K: it is taken where that is less than 2.6 us in all.
+// M x N x K of bfloat16, us in a captured graph, one kernel | two; within the rule: 2 x 2048 x 1024 3.9 | 6.7, 8 x 256 x 4096 3.9 | 6.9, 32 x 256 x 256
+// 4.7 | 5.5, 2 x 1000 x 8192 6.0 | 8.7, 8 x 1024 x 1024 5.1 | 6.7, 128 x 64 x 1024 5.2 | 7.0, 256 x 40 x 256 5.7 | 5.4; beyond it: 128 x 100 x 128 6.6 | 6.7,
+// 8 x 1024 x 2048 5.9 | 6.8, 64 x 256 x 256 7.0 | 5.6, 16 x 1024 x 512 7.0 | 6.0, 64 x 64 x 8192 8.2 | 9.2, 2 x 8192 x 1024 7.3 | 6.9.
 bool few_products(int64_t M, int64_t N, int64_t K) { return M == 1 || M * N <= 26000000 / (K + 2048); }
 
 bool known(tfjsb_dtype d) { return d == TFJSB_DTYPE_F32 || d == TFJSB_DTYPE_BF16; }
