@@ -323,7 +323,8 @@ tfjsb_status tfjsb_dropout_backprop(tfjsb_ctx* ctx, tfjsb_dtype dtype, const voi
                                     const int64_t* noise_dims, double rate, uint64_t seed, uint64_t offset, void* stream);
 
 /* Rows of x [rows,columns] as 8-bit integers with a scale each: scale = max |x| / 127, q = 127 x / max |x| rounded to nearest,
- * halves to even (decided exactly), so that q * scale is x to within half a step; a row of zeros has scale 0.  A row that holds an infinity or a NaN has that
+ * halves to even (decided exactly), so that q * scale is x to within half a step (where max |x| is below 2^-119 the scale has fewer bits than
+ * fp32's 24, below 2^-143 none are left); a row of zeros has scale 0.  A row that holds an infinity or a NaN has that
  * for a scale (NaN before infinity) and q = 0, so that products with it are NaN.  q: [rows, pitch] with pitch = columns rounded up to a
  * multiple of 16, the values past the columns zero; scale: fp32 [rows].  columns <= 131072. */
 tfjsb_status tfjsb_quantize_int8(tfjsb_ctx* ctx, tfjsb_dtype dtype, const void* x, int64_t rows, int64_t columns, int8_t* q, float* scale, void* stream);
